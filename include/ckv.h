@@ -9,8 +9,9 @@
  * Further entry points, each documented where it is declared: ckv_window_lse (the scan's first half),
  * ckv_window_utility (the first two calls as one, without the per-head masses in memory), the calls of
  * the paper's layer-shared mode (ckv_alpha_accumulate, ckv_risk_struct, ckv_shared_utility,
- * ckv_compact_kv_shared), the depth mapping of compiled tables (ckv_map_table_depth) and a decode-side consumer of the compact cache (ckv_decode_attention,
- * ckv_discarded_mass).
+ * ckv_compact_kv_shared), the depth mapping of compiled tables (ckv_map_table_depth), a decode-side consumer of the compact cache (ckv_decode_attention,
+ * ckv_discarded_mass), and the calls of a cache that goes on: norm and position rotation of new rows (ckv_norm_rotate), their way into pages
+ * (ckv_paged_append) and attention of new tokens over the pages (ckv_paged_attention).
  *
  * Notation (paper Sec. 3-4): T = prompt length (keys/values cached at the end of prefill, the
  * observation window included), W = |Omega| = observation window (the last W query positions),
@@ -362,6 +363,107 @@ ckv_status ckv_decode_attention(const ckv_params *params, const void *q_dec, int
                                 size_t workspace_bytes, void *hip_stream);
 ckv_status ckv_discarded_mass(const ckv_params *params, int32_t n_q, const float *lse_full, const float *lse_kept,
                               float *mass, float *eps_tail, void *hip_stream);
+
+/*
+ * Paged caches: lists of pages for the rows that enter a cache after (or instead of) the retention step, and attention of new tokens
+ * over them. A pool holds n_pages pages of page_rows rows for keys and one for values; a list names the pages of one (batch element,
+ * KV head) in order, so row s of the list is row s % page_rows of page table[s / page_rows]. Lists of the heads of a sequence may be
+ * one and the same (table_stride[1] = 0, pages that hold every head at k_stride[1]) or differ (retained lists of different lengths;
+ * pages of one head: k_stride[1] = v_stride[1] = 0).
+ *
+ * Of ckv_params these calls use batch, n_q_heads, n_kv_heads, head_dim, dtype and softmax_scale; seq_len is n, the most new tokens that a
+ * sequence has in the call, and q_stride / k_stride / v_stride describe the new rows q [Bz,Hq,n,d], k and v [Bz,Hkv,n,d]. The other
+ * fields have to be valid (window = 1, budget_per_kv_head = 1, cap = 1 always are) and mean nothing here.
+ *
+ *   length  in  [Bz,Hkv] int32: rows of the list with the call's new rows, which are its last ones (what is below 0 counts as 0)
+ *   count   in  [Bz,Hkv] int32 or NULL: new rows of the list, clamped to [0, n]; NULL: n. New row i is row length - count + i of
+ *               the list; rows i >= count are neither read nor written, in any tensor of the call. Query head h has the count and length of its
+ *               KV head h / G.
+ *   table   in  int32 page numbers at table_stride over (batch, KV head), max_pages in a row. A page number outside [0, n_pages),
+ *               or a row outside [0, max_pages * page_rows): nothing is written there, and attention does not see the row.
+ * A page may be in several lists (a shared prefix) as long as no call appends to it for two of them. Appending and reading are calls in
+ * stream order.
+ */
+typedef struct {
+  int32_t page_rows;       /* rows of a page, a power of two, 1 .. 65536                            */
+  int32_t n_pages;         /* pages of the pools, >= 1                                              */
+  int32_t max_pages;       /* entries of a list in `table`, >= 1; max_pages * page_rows < 2^31      */
+  int32_t reserved;        /* 0                                                                     */
+  int64_t k_stride[3];     /* element strides of k_pages over (page, KV head, row): multiples of 16 bytes, row stride >= head_dim */
+  int64_t v_stride[3];     /* the same of v_pages                                                   */
+  int64_t table_stride[2]; /* entries of `table` between batch elements, between KV heads (0: one list for all heads) */
+} ckv_pages;
+
+typedef enum { CKV_PAIR_HALVES = 0, CKV_PAIR_NEIGHBOURS = 1 } ckv_pairing;
+
+/*
+ * What happens to a row x of d components on its way: with norm != 0
+ *     y_c = x_c * weight_c / sqrt(mean_c' x_c'^2 + norm_eps)           (weight NULL: ones), else y = x,
+ * then the first rot_dim components turn by the angles a_i = position * inv_freq[i], i < rot_dim / 2, in pairs
+ *     (y_i, y_{i + rot_dim/2}) (CKV_PAIR_HALVES) or (y_{2i}, y_{2i+1}) (CKV_PAIR_NEIGHBOURS):
+ *     (y, y') -> (y cos a - y' sin a, y' cos a + y sin a).
+ * Sums and products are fp32, angles fp64 reduced to a turn; one rounding to the type at the end. With norm = 0 and rot_dim = 0
+ * rows are copied bit for bit.
+ */
+typedef struct {
+  int32_t rot_dim;   /* 0 .. head_dim, a multiple of 8                                              */
+  int32_t pairing;   /* ckv_pairing                                                                 */
+  int32_t norm;      /* 0 or 1                                                                      */
+  float norm_eps;    /* finite, >= 0                                                                */
+} ckv_rotation;
+
+/*
+ * Norm of every head of new queries and keys and their position rotation in one pass.
+ *   q, k        in   [Bz,Hq,n,d] / [Bz,Hkv,n,d] via q_stride / k_stride; either may be NULL, with its output
+ *   positions   in   [Bz,n] int32; required with rot_dim > 0
+ *   inv_freq    in   [rot_dim / 2] fp32, angle per position of each pair; required with rot_dim > 0
+ *   q_weight, k_weight  in  [d] of params->dtype, 16-byte aligned, or NULL; read only with norm
+ *   count       in   as above, or NULL
+ *   q_out, k_out  out  [Bz,Hq,n,d] / [Bz,Hkv,n,d] dense
+ * Row pointers are 16-byte aligned here and in the calls below.
+ */
+ckv_status ckv_norm_rotate(const ckv_params *params, const ckv_rotation *rotation, const void *q, const void *k,
+                           const int32_t *positions, const float *inv_freq, const void *q_weight, const void *k_weight,
+                           const int32_t *count, void *q_out, void *k_out, void *hip_stream);
+
+/*
+ * New rows into the pages: k normalised and rotated on the way, v as it is, and in the same launch q normalised and rotated to q_out
+ * (the queries of the attention that follows). rotation NULL copies k and q: rows that the retention step kept
+ * (k_out / v_out of ckv_compact_kv with its count as both length and count, strides {Hkv*cap*d, cap*d, d}, n = cap) move into pages this way.
+ *   k, v        in   [Bz,Hkv,n,d] via k_stride / v_stride
+ *   q           in   [Bz,Hq,n,d] via q_stride, or NULL with q_out = NULL
+ *   positions, inv_freq, q_weight, k_weight   as for ckv_norm_rotate. Positions are the prompt's, not places in the list:
+ *                    the retention step moves rows, their rotation stays
+ *   table, length, count           as above; length is required
+ *   k_pages, v_pages  out  new rows only, everything else in the pools stays as it is
+ *   q_out       out  [Bz,Hq,n,d] dense
+ */
+ckv_status ckv_paged_append(const ckv_params *params, const ckv_rotation *rotation, const ckv_pages *pages, const void *q,
+                            const void *k, const void *v, const int32_t *positions, const float *inv_freq, const void *q_weight,
+                            const void *k_weight, const int32_t *table, const int32_t *length, const int32_t *count,
+                            void *k_pages, void *v_pages, void *q_out, void *hip_stream);
+
+/*
+ * Attention of new tokens over the pages (the new rows included, so behind the call that appends them). New token i < count of a
+ * sequence sees the rows j <= length - count + i of its head's list that are below n_rows and whose page number is in the pool:
+ *     z[j] = softmax_scale * <q[b,h,i,:], k row j>,  lse = log sum_j exp z[j],  out = sum_j exp(z[j] - lse) * v row j
+ * What a token does not see has no influence, whatever it holds (infinities and NaN included). A token that sees no row gets zeros and
+ * lse = -inf. With n = 1 this is a decoding step; lse of a prompt's last W tokens is the `lse` of
+ * ckv_window_scores, lse of two caches is what ckv_discarded_mass takes.
+ *   n_rows      no list is longer, 1 .. max_pages * page_rows and at most 2^24; a bound near the lengths lets the call share its work out well
+ *   q           in   [Bz,Hq,n,d] via q_stride
+ *   out         out  [Bz,Hq,n,d] of params->dtype at element strides out_stride over (batch, query head, token), multiples of 16 bytes,
+ *                    or dense (out_stride NULL)
+ *   lse         out  [Bz,Hq,n] fp32, natural log, or NULL
+ *   workspace        ckv_paged_workspace_bytes(params, n_rows) bytes, 256-byte aligned; NULL where that is 0 (it is for refused arguments
+ *                    too). Contents undefined before and after.
+ * Logits and sums are fp32; in bf16 the weights enter the second product rounded to bf16, as the output is.
+ */
+size_t ckv_paged_workspace_bytes(const ckv_params *params, int32_t n_rows);
+ckv_status ckv_paged_attention(const ckv_params *params, const ckv_pages *pages, const void *q, const void *k_pages,
+                               const void *v_pages, const int32_t *table, const int32_t *length, const int32_t *count, int32_t n_rows,
+                               void *out, const int64_t *out_stride, float *lse, void *workspace, size_t workspace_bytes,
+                               void *hip_stream);
 
 /* Static text for a status code; never NULL. */
 const char *ckv_status_string(ckv_status status);

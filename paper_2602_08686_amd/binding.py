@@ -1,4 +1,4 @@
-"""ctypes binding of libckv.so: the same four calls as ``include/ckv.h``, argument marshalling only.
+"""ctypes binding of libckv.so: the same calls as ``include/ckv.h``, argument marshalling only.
 
 PyTorch supplies device memory and the current HIP stream; every step of the retention path runs in
 the library's kernels. There is no fallback: if the library is missing, loading raises.
@@ -18,11 +18,13 @@ CKV_OK, CKV_EINVAL, CKV_EUNSUPPORTED, CKV_EWORKSPACE, CKV_EHIP = range(5)
 CKV_F32, CKV_BF16 = 0, 1
 POOL_NONE, POOL_AVG, POOL_MAX = 0, 1, 2
 FLAG_VALUE_NORM = 1
+PAIR_HALVES, PAIR_NEIGHBOURS = 0, 1   # components of a row that turn together (ckv_rotation)
 FLAG_GROUP_MASS = 8         # ckv_window_scores writes per-KV-head sums [Bz,Hkv,T] (layer-shared mode)
 
 EXPORTS = ("ckv_workspace_bytes", "ckv_window_lse", "ckv_window_lse_static_bytes", "ckv_window_lse_static", "ckv_window_scores", "ckv_window_utility", "ckv_apply_tables", "ckv_select_topk",
            "ckv_compact_kv", "ckv_retention_layer", "ckv_alpha_accumulate", "ckv_risk_struct", "ckv_shared_utility", "ckv_compact_kv_shared",
            "ckv_decode_workspace_bytes", "ckv_decode_attention", "ckv_discarded_mass", "ckv_map_table_depth",
+           "ckv_norm_rotate", "ckv_paged_append", "ckv_paged_workspace_bytes", "ckv_paged_attention",
            "ckv_status_string")
 
 
@@ -36,6 +38,17 @@ class CkvParams(ctypes.Structure):
         ("pool", ctypes.c_int32), ("pool_kernel", ctypes.c_int32),
         ("budget_per_kv_head", ctypes.c_int32), ("cap", ctypes.c_int32), ("flags", ctypes.c_uint32),
     ]
+
+
+class CkvPages(ctypes.Structure):
+    _fields_ = [
+        ("page_rows", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3), ("table_stride", ctypes.c_int64 * 2),
+    ]
+
+
+class CkvRotation(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("pairing", ctypes.c_int32), ("norm", ctypes.c_int32), ("norm_eps", ctypes.c_float)]
 
 
 class CkvError(RuntimeError):
@@ -93,6 +106,15 @@ def load(path: Optional[Path] = None):
     lib.ckv_decode_attention.restype = ctypes.c_int
     lib.ckv_discarded_mass.argtypes = [pp, ctypes.c_int32, vp, vp, vp, vp, vp]
     lib.ckv_discarded_mass.restype = ctypes.c_int
+    gp, rp = ctypes.POINTER(CkvPages), ctypes.POINTER(CkvRotation)
+    lib.ckv_norm_rotate.argtypes = [pp, rp] + [vp] * 10
+    lib.ckv_norm_rotate.restype = ctypes.c_int
+    lib.ckv_paged_append.argtypes = [pp, rp, gp] + [vp] * 14
+    lib.ckv_paged_append.restype = ctypes.c_int
+    lib.ckv_paged_workspace_bytes.argtypes = [pp, ctypes.c_int32]
+    lib.ckv_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.ckv_paged_attention.argtypes = [pp, gp, vp, vp, vp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.ckv_paged_attention.restype = ctypes.c_int
     lib.ckv_map_table_depth.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, vp, ctypes.c_int32, vp]
     lib.ckv_map_table_depth.restype = ctypes.c_int
     lib.ckv_status_string.argtypes = [ctypes.c_int]
@@ -268,6 +290,78 @@ def ckv_decode_attention(params, q_dec, k_rows, v_rows, count, out, lse, workspa
 def ckv_discarded_mass(params, n_q, lse_full, lse_kept, mass, eps_tail=None, stream=None):
     _check(load().ckv_discarded_mass(ctypes.byref(params), int(n_q), _ptr(lse_full), _ptr(lse_kept), _ptr(mass),
                                      _ptr(eps_tail), _stream(stream)), "ckv_discarded_mass")
+
+
+def _row_strides(t: torch.Tensor, d: int):
+    """Element strides over the first three axes of [.., .., .., d]; an axis of one entry has whatever stride suits the library."""
+    return [s if n > 1 else d for n, s in zip(t.shape[:3], t.stride()[:3])]
+
+
+def step_params(*, q=None, k=None, v=None, n_q_heads, n_kv_heads, softmax_scale=0.0) -> CkvParams:
+    """ckv_params of a call on new tokens: q [Bz,Hq,n,d], k and v [Bz,Hkv,n,d] (any strides with a contiguous last axis); those
+    that the call does not have are None."""
+    one = next((t for t in (q, k, v) if t is not None), None)
+    if one is None:
+        raise ValueError("step_params needs one of q, k and v")
+    batch, _, n, d = one.shape
+    for name, t, heads in (("q", q, n_q_heads), ("k", k, n_kv_heads), ("v", v, n_kv_heads)):
+        if t is not None and (tuple(t.shape) != (batch, heads, n, d) or t.stride(3) != 1 or t.dtype != one.dtype):
+            raise ValueError(f"{name} has to be [{batch},{heads},{n},{d}] of one type with a contiguous last axis")
+    strides = {f"{name}_stride": None if t is None else _row_strides(t, d) for name, t in (("q", q), ("k", k), ("v", v))}
+    strides["q_stride"] = strides["q_stride"] or (n_q_heads * n * d, n * d, d)
+    return make_params(batch=batch, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=d, seq_len=n, window=1, dtype=one.dtype,
+                       pool=POOL_NONE, pool_kernel=1, budget=1, cap=1, softmax_scale=softmax_scale, **strides)
+
+
+def make_rotation(rot_dim, *, pairing=PAIR_HALVES, norm=False, norm_eps=1e-6) -> CkvRotation:
+    return CkvRotation(int(rot_dim), int(pairing), int(bool(norm)), float(norm_eps))
+
+
+def pages_for(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor) -> CkvPages:
+    """ckv_pages of pools [n_pages,Hkv,page_rows,d] (any strides with a contiguous last axis; pages of one head are handed over as an
+    expanded view) and of lists [Bz,max_pages] (one for all heads of a sequence) or [Bz,Hkv,max_pages]."""
+    if k_pages.shape != v_pages.shape or k_pages.dim() != 4 or k_pages.stride(3) != 1 or v_pages.stride(3) != 1:
+        raise ValueError("k_pages and v_pages have to be [n_pages,Hkv,page_rows,d] with a contiguous last axis")
+    if table.dtype != torch.int32 or table.dim() not in (2, 3) or (table.shape[-1] > 1 and table.stride(-1) != 1):
+        raise ValueError("table has to be int32 [Bz,max_pages] or [Bz,Hkv,max_pages] with a contiguous last axis")
+    p, d = CkvPages(), k_pages.shape[3]
+    p.n_pages, p.page_rows, p.max_pages = k_pages.shape[0], k_pages.shape[2], table.shape[-1]
+    for name, t in (("k_stride", k_pages), ("v_stride", v_pages)):
+        arr = getattr(p, name)
+        for i, s in enumerate(_row_strides(t, d)):
+            arr[i] = int(s)
+    p.table_stride[0] = table.stride(0)
+    p.table_stride[1] = table.stride(1) if table.dim() == 3 else 0
+    return p
+
+
+def ckv_norm_rotate(params, rotation, q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out, count=None, stream=None):
+    _check(load().ckv_norm_rotate(ctypes.byref(params), ctypes.byref(rotation), _ptr(q), _ptr(k), _ptr(positions), _ptr(inv_freq),
+                                  _ptr(q_weight), _ptr(k_weight), _ptr(count), _ptr(q_out), _ptr(k_out), _stream(stream)),
+           "ckv_norm_rotate")
+
+
+def ckv_paged_append(params, rotation, pages, k, v, k_pages, v_pages, table, length, count=None, positions=None, inv_freq=None,
+                     k_weight=None, q=None, q_weight=None, q_out=None, stream=None):
+    """rotation may be None: plain copies (rows that the retention step kept)."""
+    _check(load().ckv_paged_append(ctypes.byref(params), None if rotation is None else ctypes.byref(rotation), ctypes.byref(pages),
+                                   _ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight),
+                                   _ptr(table), _ptr(length), _ptr(count), _ptr(k_pages), _ptr(v_pages), _ptr(q_out),
+                                   _stream(stream)), "ckv_paged_append")
+
+
+def ckv_paged_workspace_bytes(params, n_rows) -> int:
+    return int(load().ckv_paged_workspace_bytes(ctypes.byref(params), int(n_rows)))
+
+
+def ckv_paged_attention(params, pages, q, k_pages, v_pages, table, length, n_rows, out, lse=None, workspace=None, count=None,
+                        stream=None):
+    """out [Bz,Hq,n,d], any strides over the first three axes."""
+    strides = None if out.is_contiguous() else (ctypes.c_int64 * 3)(*_row_strides(out, out.shape[3]))
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load().ckv_paged_attention(ctypes.byref(params), ctypes.byref(pages), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table),
+                                      _ptr(length), _ptr(count), int(n_rows), _ptr(out), strides, _ptr(lse), _ptr(workspace), nbytes,
+                                      _stream(stream)), "ckv_paged_attention")
 
 
 class LayerBuffers:

@@ -6,9 +6,10 @@
 
 #include <atomic>
 #include <chrono>
+#include <initializer_list>
 #include <mutex>
 
-#include "ckv_internal.h"
+#include "ckv_pages.h"
 
 namespace ckv {
 
@@ -652,6 +653,116 @@ extern "C" ckv_status ckv_discarded_mass(const ckv_params *params, int32_t n_q, 
   Shape s;
   derive(params, &s);
   if (launch_discarded_mass(s, n_q, lse_full, lse_kept, mass, eps_tail, (hipStream_t)hip_stream) != hipSuccess)
+    return CKV_EHIP;
+  return CKV_OK;
+}
+
+static ckv_status rotation_refused(const ckv_params *p, const ckv_rotation *r, const int32_t *positions, const float *inv_freq) {
+  if (!r) return CKV_OK;
+  if (r->rot_dim < 0 || r->rot_dim > p->head_dim || r->rot_dim % 2) return CKV_EINVAL;
+  if (r->pairing != CKV_PAIR_HALVES && r->pairing != CKV_PAIR_NEIGHBOURS) return CKV_EINVAL;
+  if ((r->norm != 0 && r->norm != 1) || !(r->norm_eps >= 0.0f) || isinf(r->norm_eps)) return CKV_EINVAL;
+  if (r->rot_dim > 0 && (!positions || !inv_freq)) return CKV_EINVAL;
+  if (r->rot_dim % 8) return CKV_EUNSUPPORTED;
+  return CKV_OK;
+}
+
+static ckv_status pages_refused(const ckv_params *p, const ckv_pages *g) {
+  if (!g || g->page_rows < 1 || g->n_pages < 1 || g->max_pages < 1 || g->reserved != 0) return CKV_EINVAL;
+  const int64_t per16 = p->dtype == CKV_BF16 ? 8 : 4;
+  for (int i = 0; i < 3; ++i)
+    if (g->k_stride[i] < 0 || g->v_stride[i] < 0 || g->k_stride[i] % per16 || g->v_stride[i] % per16) return CKV_EINVAL;
+  if (g->k_stride[2] < p->head_dim || g->v_stride[2] < p->head_dim) return CKV_EINVAL;
+  if (g->n_pages > 1 && (g->k_stride[0] < p->head_dim || g->v_stride[0] < p->head_dim)) return CKV_EINVAL;
+  if (g->table_stride[0] < 0 || g->table_stride[1] < 0) return CKV_EINVAL;
+  if (g->page_rows > 65536 || (g->page_rows & (g->page_rows - 1))) return CKV_EUNSUPPORTED;
+  if ((int64_t)g->page_rows * g->max_pages > INT32_MAX) return CKV_EUNSUPPORTED;
+  return CKV_OK;
+}
+
+static bool misaligned(std::initializer_list<const void *> pointers) {
+  uintptr_t all = 0;
+  for (const void *p : pointers) all |= (uintptr_t)p;
+  return all & 15;
+}
+
+extern "C" ckv_status ckv_norm_rotate(const ckv_params *params, const ckv_rotation *rotation, const void *q, const void *k,
+                                      const int32_t *positions, const float *inv_freq, const void *q_weight, const void *k_weight,
+                                      const int32_t *count, void *q_out, void *k_out, void *hip_stream) {
+  ckv_status st = validate(params);
+  if (st != CKV_OK) return st;
+  if (!rotation || (!q && !k) || !q != !q_out || !k != !k_out) return CKV_EINVAL;
+  if (misaligned({q, k, q_weight, k_weight, q_out, k_out})) return CKV_EINVAL;
+  st = rotation_refused(params, rotation, positions, inv_freq);
+  if (st != CKV_OK) return st;
+  if ((int64_t)params->batch * params->seq_len > INT32_MAX / 16) return CKV_EUNSUPPORTED;  // workgroups of a launch
+  Shape s;
+  derive(params, &s);
+  if (launch_rows(params, s, rotation, nullptr, q, k, nullptr, positions, inv_freq, q_weight, k_weight, nullptr, nullptr, count, q_out,
+                  k_out, nullptr, (hipStream_t)hip_stream) != hipSuccess)
+    return CKV_EHIP;
+  return CKV_OK;
+}
+
+extern "C" ckv_status ckv_paged_append(const ckv_params *params, const ckv_rotation *rotation, const ckv_pages *pages, const void *q,
+                                       const void *k, const void *v, const int32_t *positions, const float *inv_freq,
+                                       const void *q_weight, const void *k_weight, const int32_t *table, const int32_t *length,
+                                       const int32_t *count, void *k_pages, void *v_pages, void *q_out, void *hip_stream) {
+  ckv_status st = validate(params);
+  if (st != CKV_OK) return st;
+  if (!k || !v || !table || !length || !k_pages || !v_pages || !q != !q_out) return CKV_EINVAL;
+  if (misaligned({q, k, v, q_weight, k_weight, k_pages, v_pages, q_out})) return CKV_EINVAL;
+  st = rotation_refused(params, rotation, positions, inv_freq);
+  if (st == CKV_OK) st = pages_refused(params, pages);
+  if (st != CKV_OK) return st;
+  if ((int64_t)params->batch * params->seq_len > INT32_MAX / 16) return CKV_EUNSUPPORTED;
+  Shape s;
+  derive(params, &s);
+  if (launch_rows(params, s, rotation, pages, q, k, v, positions, inv_freq, q_weight, k_weight, table, length, count, q_out, k_pages,
+                  v_pages, (hipStream_t)hip_stream) != hipSuccess)
+    return CKV_EHIP;
+  return CKV_OK;
+}
+
+static ckv_status paged_size_refused(int32_t n_rows) {
+  if (n_rows < 1) return CKV_EINVAL;
+  if (n_rows > (1 << 24)) return CKV_EUNSUPPORTED;
+  return CKV_OK;
+}
+
+extern "C" size_t ckv_paged_workspace_bytes(const ckv_params *params, int32_t n_rows) {
+  if (validate(params) != CKV_OK || paged_size_refused(n_rows) != CKV_OK) return 0;
+  Shape s;
+  derive(params, &s);
+  const PagedPlan plan = plan_paged(s, n_rows);
+  return plan.workgroups > kMostPagedWorkgroups ? 0 : align256(plan.workspace_bytes);
+}
+
+extern "C" ckv_status ckv_paged_attention(const ckv_params *params, const ckv_pages *pages, const void *q, const void *k_pages,
+                                          const void *v_pages, const int32_t *table, const int32_t *length, const int32_t *count,
+                                          int32_t n_rows, void *out, const int64_t *out_stride, float *lse, void *workspace,
+                                          size_t workspace_bytes, void *hip_stream) {
+  ckv_status st = validate(params);
+  if (st != CKV_OK) return st;
+  if (!q || !k_pages || !v_pages || !table || !length || !out) return CKV_EINVAL;
+  if (misaligned({q, k_pages, v_pages, out})) return CKV_EINVAL;
+  st = pages_refused(params, pages);
+  if (st == CKV_OK) st = paged_size_refused(n_rows);
+  if (st != CKV_OK) return st;
+  if (n_rows > pages->page_rows * pages->max_pages) return CKV_EINVAL;
+  if (out_stride) {
+    const int64_t per16 = params->dtype == CKV_BF16 ? 8 : 4;
+    for (int i = 0; i < 3; ++i)
+      if (out_stride[i] < params->head_dim || out_stride[i] % per16) return CKV_EINVAL;
+  }
+  Shape s;
+  derive(params, &s);
+  const PagedPlan plan = plan_paged(s, n_rows);
+  if (plan.workgroups > kMostPagedWorkgroups) return CKV_EUNSUPPORTED;
+  if (plan.workspace_bytes > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < plan.workspace_bytes))
+    return CKV_EWORKSPACE;
+  if (launch_paged_attention(params, s, plan, pages, q, k_pages, v_pages, table, length, count, n_rows, out, out_stride, lse,
+                             (char *)workspace, (hipStream_t)hip_stream) != hipSuccess)
     return CKV_EHIP;
   return CKV_OK;
 }

@@ -156,6 +156,47 @@ void mfma_16x16x32_bf16(const void *x, const void *y, const float *c, float *d) 
   }
 }
 
+void mfma_32x32x16_bf16(const void *x, const void *y, const float *c, float *d) {
+  char both[32];
+  memcpy(both, x, 16);
+  memcpy(both + 16, y, 16);
+  const char *all = static_cast<const char *>(exchange(both, sizeof both));
+  const auto at = [&](int l, int which, int i) {
+    uint16_t h;
+    memcpy(&h, all + 64 * l + 16 * which + 2 * i, sizeof h);
+    return (double)__builtin_bit_cast(float, (uint32_t)h << 16);
+  };
+  const int col = lane() % 32, half = lane() / 32;
+  for (int r = 0; r < 16; ++r) {
+    const int row = 8 * (r / 4) + 4 * half + r % 4;
+    double s = c[r];
+    for (int k = 0; k < 2; ++k)
+      for (int i = 0; i < 8; ++i) s += at(32 * k + row, 0, i) * at(32 * k + col, 1, i);
+    d[r] = (float)s;
+  }
+}
+
+void mfma_32x32x2_f32(float x, float y, const float *c, float *d) {
+  const float both[2] = {x, y};
+  const char *all = static_cast<const char *>(exchange(both, sizeof both));
+  const auto at = [&](int l, int which) {
+    float f;
+    memcpy(&f, all + 64 * l + 4 * which, sizeof f);
+    return (double)f;
+  };
+  const int col = lane() % 32, half = lane() / 32;
+  for (int r = 0; r < 16; ++r) {
+    const int row = 8 * (r / 4) + 4 * half + r % 4;
+    d[r] = (float)(c[r] + at(row, 0) * at(col, 1) + at(32 + row, 0) * at(32 + col, 1));
+  }
+}
+
+void read_transposed(const void *four_words, void *out) {
+  const char *all = static_cast<const char *>(exchange(four_words, 8));
+  const int l = lane(), first = l & ~15, i = l & 15;
+  for (int k = 0; k < 4; ++k) memcpy(static_cast<char *>(out) + 2 * k, all + 64 * (first + 4 * k + i / 4) + 2 * (i % 4), 2);
+}
+
 void launch(dim3 grid, dim3 block, const std::function<void()> &body) {
   const int n = (int)block.x;
   if (!stacks) stacks = static_cast<char *>(mmap(nullptr, kStack * 1024, PROT_READ | PROT_WRITE, MAP_PRIVATE | MAP_ANONYMOUS, -1, 0));

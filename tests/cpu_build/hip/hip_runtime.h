@@ -28,6 +28,8 @@ struct float2 { float x, y; };
 struct int2 { int x, y; };
 struct alignas(16) int4 { int x, y, z, w; };
 struct alignas(16) uint4 { uint32_t x, y, z, w; };
+struct uint2 { uint32_t x, y; };
+inline uint2 make_uint2(uint32_t x, uint32_t y) { return {x, y}; }
 inline float2 make_float2(float x, float y) { return {x, y}; }
 inline int2 make_int2(int x, int y) { return {x, y}; }
 inline uint4 make_uint4(uint32_t x, uint32_t y, uint32_t z, uint32_t w) { return {x, y, z, w}; }
@@ -60,6 +62,9 @@ struct Pair {
 Pair swap_halves(uint32_t x, uint32_t y, int width);
 int update_dpp(int old, int src, int ctrl, int row_mask);
 void mfma_16x16x32_bf16(const void *x, const void *y, const float *c, float *d);
+void mfma_32x32x16_bf16(const void *x, const void *y, const float *c, float *d);
+void mfma_32x32x2_f32(float x, float y, const float *c, float *d);
+void read_transposed(const void *four_words, void *out);  // of 16 bits, among 16 lanes
 }  // namespace emu
 
 #define threadIdx emu::thread_idx
@@ -117,6 +122,32 @@ template <class V, class F> F mfma_16x16x32(const V &x, const V &y, F acc) {
   F out;
   emu::mfma_16x16x32_bf16(&x, &y, reinterpret_cast<const float *>(&acc), reinterpret_cast<float *>(&out));
   return out;
+}
+template <class V, class F> F mfma_32x32x16(const V &x, const V &y, F acc) {
+  F out;
+  emu::mfma_32x32x16_bf16(&x, &y, reinterpret_cast<const float *>(&acc), reinterpret_cast<float *>(&out));
+  return out;
+}
+template <class F> F mfma_32x32x2(float x, float y, F acc) {
+  F out;
+  emu::mfma_32x32x2_f32(x, y, reinterpret_cast<const float *>(&acc), reinterpret_cast<float *>(&out));
+  return out;
+}
+#define __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, acc, a, b, c) mfma_32x32x16(x, y, acc)
+#define __builtin_amdgcn_mfma_f32_32x32x2f32(x, y, acc, a, b, c) mfma_32x32x2(x, y, acc)
+template <class P> auto read_tr16(P at) {  // P: a pointer to four words in LDS
+  typedef __attribute__((ext_vector_type(4))) short words;
+  words out;
+  emu::read_transposed((const void *)at, &out);
+  return out;
+}
+#define __builtin_amdgcn_ds_read_tr16_b64_v4i16(at) read_tr16(at)
+// There at once: what the wait is for does not show here.
+#define __builtin_amdgcn_global_load_lds(from, lds, bytes, offset, aux) memcpy((char *)(lds) + (bytes) * emu::lane(), (const void *)(from), bytes)
+#define __builtin_amdgcn_s_waitcnt(x) ((void)0)
+inline void sincospif(float x, float *s, float *c) {
+  *s = (float)sin(3.14159265358979323846 * (double)x);
+  *c = (float)cos(3.14159265358979323846 * (double)x);
 }
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, acc, a, b, c) mfma_16x16x32(x, y, acc)
 
