@@ -167,6 +167,11 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+def _at(t: Optional[torch.Tensor]):
+    """A tensor's address as ctypes takes it for a void pointer: without an object for each, which is most of a short call's host time."""
+    return None if t is None else t.data_ptr()
+
+
 def _stream(stream) -> ctypes.c_void_p:
     """The given stream's handle, or the current stream's of the current device. Asked of the runtime directly: a
     torch.cuda.Stream object for it costs 3 us per call, as much as the launch (a gather call: 7.7 us of host time -> 4.5)."""
@@ -336,8 +341,8 @@ def pages_for(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor)
 
 
 def ckv_norm_rotate(params, rotation, q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out, count=None, stream=None):
-    _check(load().ckv_norm_rotate(ctypes.byref(params), ctypes.byref(rotation), _ptr(q), _ptr(k), _ptr(positions), _ptr(inv_freq),
-                                  _ptr(q_weight), _ptr(k_weight), _ptr(count), _ptr(q_out), _ptr(k_out), _stream(stream)),
+    _check(load().ckv_norm_rotate(ctypes.byref(params), ctypes.byref(rotation), _at(q), _at(k), _at(positions), _at(inv_freq),
+                                  _at(q_weight), _at(k_weight), _at(count), _at(q_out), _at(k_out), _stream(stream)),
            "ckv_norm_rotate")
 
 
@@ -345,8 +350,8 @@ def ckv_paged_append(params, rotation, pages, k, v, k_pages, v_pages, table, len
                      k_weight=None, q=None, q_weight=None, q_out=None, stream=None):
     """rotation may be None: plain copies (rows that the retention step kept)."""
     _check(load().ckv_paged_append(ctypes.byref(params), None if rotation is None else ctypes.byref(rotation), ctypes.byref(pages),
-                                   _ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight),
-                                   _ptr(table), _ptr(length), _ptr(count), _ptr(k_pages), _ptr(v_pages), _ptr(q_out),
+                                   _at(q), _at(k), _at(v), _at(positions), _at(inv_freq), _at(q_weight), _at(k_weight),
+                                   _at(table), _at(length), _at(count), _at(k_pages), _at(v_pages), _at(q_out),
                                    _stream(stream)), "ckv_paged_append")
 
 
@@ -359,8 +364,8 @@ def ckv_paged_attention(params, pages, q, k_pages, v_pages, table, length, n_row
     """out [Bz,Hq,n,d], any strides over the first three axes."""
     strides = None if out.is_contiguous() else (ctypes.c_int64 * 3)(*_row_strides(out, out.shape[3]))
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(load().ckv_paged_attention(ctypes.byref(params), ctypes.byref(pages), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table),
-                                      _ptr(length), _ptr(count), int(n_rows), _ptr(out), strides, _ptr(lse), _ptr(workspace), nbytes,
+    _check(load().ckv_paged_attention(ctypes.byref(params), ctypes.byref(pages), _at(q), _at(k_pages), _at(v_pages), _at(table),
+                                      _at(length), _at(count), int(n_rows), _at(out), strides, _at(lse), _at(workspace), nbytes,
                                       _stream(stream)), "ckv_paged_attention")
 
 
@@ -390,7 +395,7 @@ def retention_layer(params: CkvParams, q, k, v, tables: dict, buf: LayerBuffers,
     """Queues the kernels of one layer back-to-back on the stream, by one call of the library; returns nothing (outputs in
     buf). fused_utility: those of ckv_window_utility in place of ckv_window_scores + ckv_apply_tables (buf.scores is
     then scratch)."""
-    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    at = _at
     get, ws = tables.get, buf.workspace
     _check(load().ckv_retention_layer(
         ctypes.byref(params), at(q), at(k), at(v), at(lse), at(tables["w_head"]), at(get("head_share")), at(get("t_gate")),

@@ -1,0 +1,287 @@
+// What the kernels of ckv_paged_attention share (private): the matrix forms of the two products, and how a call is shared out.
+#ifndef CKV_PAGED_H_
+#define CKV_PAGED_H_
+
+#include <type_traits>
+
+#include "ckv_pages.h"
+#include <ckv_dma.h>
+
+namespace ckv {
+
+struct PagedArgs {
+  const char *q, *k, *v;
+  int64_t qs[3];       // BYTES between batch elements, query heads, tokens
+  PageLists lists;
+  char *out;
+  int64_t os[3];       // BYTES, as qs
+  float *lse;          // [Bz][Hq][n] natural log, or null
+  float *part;         // [unit][column tile][chunk][column of the tile][d]: weighted sums of V
+  float2 *stats;       // [unit][column tile][chunk][column of the tile]: running maximum (log2), sum
+  int Hq, Hkv, G, n, n_rows;
+  int tile_cols, col_tiles, stage_rows, n_chunks, workgroups;  // of the plan
+  float scale2;        // softmax scale * log2(e)
+};
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_p;
+typedef __attribute__((ext_vector_type(16))) float f32x16_p;
+typedef __attribute__((ext_vector_type(4))) float f32x4_p;
+typedef __attribute__((ext_vector_type(4))) short s16x4_p;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_p;
+
+constexpr int kXcdsP = 8;  // accelerator dies of the part; workgroup i of a launch runs on die i % 8
+
+// Four 16-bit words a lane, transposed among 16 lanes: lane i gets word i % 4 of what lanes i / 4, 4 + i / 4, 8 + i / 4, 12 + i / 4 read.
+__device__ __forceinline__ u32x2_p read_transposed(const char *lds) {
+  typedef __attribute__((address_space(3))) s16x4_p lds_words;
+  return __builtin_bit_cast(u32x2_p, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_words *)lds));
+}
+
+// Rows as they lie in LDS: one behind the other, the 16-byte pieces of a row permuted so that what one cycle reads (16 bytes of eight
+// rows of K, 32 bytes of four rows of V) lies in different banks. Both permutations are their own inverses.
+template <int DT, int DH>
+struct Image {
+  static constexpr int ROW = DH * (DT == CKV_BF16 ? 2 : 4);  // bytes
+  static constexpr int PIECES = ROW / 16;
+  static constexpr int ROWS_PER_LOAD = 1024 / ROW;           // a wave's load of 16 bytes a lane
+  static constexpr int STEPS = PIECES / 2;                   // pieces of a row per half of the wave
+  static constexpr int DTILES = DH / 32;
+  static __device__ __forceinline__ int k_piece(int r, int c) { return c ^ (r & 7); }
+  static __device__ __forceinline__ int v_piece(int r, int c) {
+    if (DT != CKV_BF16) return c;  // a cycle reads 32 lanes' words of one row
+    return c ^ (2 * (ROW == 128 ? (r >> 1) & 3 : r & 3));
+  }
+};
+
+// The rows that a tile's columns see, and how its chunks share them: whole stages.
+struct TileRange {
+  int cols;  // columns of the tile that exist
+  int end;   // rows that the last of them sees
+  int stages, per_chunk;
+};
+__device__ __forceinline__ TileRange tile_range(const PagedArgs &a, int unit, int tile) {
+  TileRange t;
+  const int count = new_rows(a.lists, unit, a.n), length = max(a.lists.length[unit], 0);
+  t.cols = min(a.G * count - tile * a.tile_cols, a.tile_cols);
+  const int last = (tile * a.tile_cols + t.cols - 1) / a.G;
+  t.end = t.cols > 0 ? min(max(length - count + last + 1, 0), a.n_rows) : 0;
+  t.stages = (t.end + a.stage_rows - 1) / a.stage_rows;
+  t.per_chunk = max(1, (t.stages + a.n_chunks - 1) / a.n_chunks);
+  return t;
+}
+
+// Column `local` of a tile: a token and one of the group's heads.
+struct Column {
+  int token, h;
+  int limit;  // rows that it sees
+};
+__device__ __forceinline__ Column column(const PagedArgs &a, int unit, int tile, int local) {
+  const int col = tile * a.tile_cols + local, g = unit % a.Hkv;
+  Column c;
+  c.token = col / a.G;
+  c.h = g * a.G + col - c.token * a.G;
+  c.limit = min(max(max(a.lists.length[unit], 0) - new_rows(a.lists, unit, a.n) + c.token + 1, 0), a.n_rows);
+  return c;
+}
+
+// Workgroup `id` of a launch: XCD id % 8 gets a contiguous part of the work, so that the workgroups that read the same
+// rows at the same time share an L2.
+__device__ __forceinline__ int work_item(int id, int total) {
+  const int xcd = id % kXcdsP, at = id / kXcdsP, each = total / kXcdsP, more = total % kXcdsP;
+  return xcd * each + min(xcd, more) + at;
+}
+
+// Over the two lanes (l, l ^ 32) that share a column.
+template <class Op>
+__device__ __forceinline__ float over_halves(float x, Op op) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// A column's operand of the first product: pieces 2 s + half of its query row.
+template <int DT, int DH>
+__device__ __forceinline__ void load_query(const PagedArgs &a, int b, const Column &c, bool valid, int half, u32x4_d (&qf)[Image<DT, DH>::STEPS]) {
+#pragma unroll
+  for (int s = 0; s < Image<DT, DH>::STEPS; ++s) {
+    qf[s] = u32x4_d{0u, 0u, 0u, 0u};
+    if (valid) qf[s] = *reinterpret_cast<const u32x4_d *>(a.q + b * a.qs[0] + c.h * a.qs[1] + c.token * a.qs[2] + (2 * s + half) * 16);
+  }
+}
+
+// Eight (bf16) or four (f32) contraction indexes of each half of the wave.
+template <int DT>
+__device__ __forceinline__ void mma_piece(f32x16_p &acc, const u32x4_d &x, const u32x4_d &y) {
+  if (DT == CKV_BF16) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_p, x), __builtin_bit_cast(bf16x8_p, y), acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(y[e]), acc, 0, 0, 0);
+  }
+}
+
+// First product of 32 rows of K: element r is the product of row block_row(r, half) with the lane's column (lane % 32).
+__device__ __forceinline__ int block_row(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
+template <int DT, int DH>
+__device__ __forceinline__ void first_product(const char *image, int lane, const u32x4_d (&qf)[Image<DT, DH>::STEPS], f32x16_p &z) {
+  typedef Image<DT, DH> I;
+  const int row = lane & 31, half = lane >> 5;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.0f;
+#pragma unroll
+  for (int s = 0; s < I::STEPS; ++s)
+    mma_piece<DT>(z, *reinterpret_cast<const u32x4_d *>(image + row * I::ROW + I::k_piece(row, 2 * s + half) * 16), qf[s]);
+}
+
+// How a second sweep takes V's components: ones where there is an infinity of one sign or a NaN, or the finite ones only.
+enum VMode { kUp, kDown, kFinite };
+template <int DT>
+__device__ __forceinline__ uint32_t v_word(uint32_t x, int mode) {
+  if (DT == CKV_BF16) {
+    uint32_t out = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t b = (x >> (16 * h)) & 0xffffu;
+      const bool finite = (b & 0x7f80u) != 0x7f80u, nan = !finite && (b & 0x7fu);
+      const bool marked = !finite && (nan || (mode == kUp) == !(b & 0x8000u));
+      out |= (mode == kFinite ? (finite ? b : 0u) : (marked ? 0x3f80u : 0u)) << (16 * h);
+    }
+    return out;
+  }
+  const bool finite = (x & 0x7f800000u) != 0x7f800000u, nan = !finite && (x & 0x7fffffu);
+  const bool marked = !finite && (nan || (mode == kUp) == !(x & 0x80000000u));
+  return mode == kFinite ? (finite ? x : 0u) : (marked ? 0x3f800000u : 0u);
+}
+
+// Second product of 32 rows of V with the weights w (as the first product left the logits): component 32 t + block_row(r, half) of the lane's
+// column is acc[t][r]. CAREFUL: V's components as `mode` says. In bf16 the weights are rounded to the type, to the nearest: 2^-9 of each on
+// average, of both signs, which over many rows is less than the output's own rounding.
+template <int DT, int DH, bool CAREFUL>
+__device__ __forceinline__ void second_product(const char *image, int lane, const f32x16_p &w, f32x16_p (&acc)[DH / 32], int mode) {
+  typedef Image<DT, DH> I;
+  const int half = lane >> 5;
+  if constexpr (DT == CKV_BF16) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      u32x4_d y;  // weights of rows 16 j + 4 half + (0..3), and of those eight further on
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = pack_bf16(w[8 * j + 2 * e], w[8 * j + 2 * e + 1]);
+#pragma unroll
+      for (int t = 0; t < I::DTILES; ++t) {
+        u32x4_d x;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          // 16 lanes read four rows of 16 components and get a component's four rows each
+          const int row = 16 * j + 8 * p + 4 * half + (lane & 15) / 4;
+          const int byte = 64 * t + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+          const u32x2_p two = read_transposed(image + row * I::ROW + I::v_piece(row, byte / 16) * 16 + byte % 16);
+          x[2 * p] = two[0];
+          x[2 * p + 1] = two[1];
+        }
+        if (CAREFUL)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = v_word<DT>(x[e], mode);
+        mma_piece<DT>(acc[t], x, y);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int row = block_row(r, half);
+#pragma unroll
+      for (int t = 0; t < I::DTILES; ++t) {
+        uint32_t x = *reinterpret_cast<const uint32_t *>(image + row * I::ROW + (32 * t + (lane & 31)) * 4);
+        if (CAREFUL) x = v_word<DT>(x, mode);
+        acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x), w[r], acc[t], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// Online softmax of a lane's column: the running maximum (log2 domain, common to both halves of the wave) and the sum of this half's rows.
+struct Running {
+  float top, sum;
+};
+// Logits to weights. A new maximum scales what there is: rare after the first blocks. CAREFUL with a mode other than kFinite: the weights become ones.
+template <int BLOCKS, int DTILES, bool CAREFUL>
+__device__ __forceinline__ void online_softmax(f32x16_p (&z)[BLOCKS], float scale2, Running &run, f32x16_p (&acc)[DTILES], int mode) {
+  float mx = z[0][0];
+#pragma unroll
+  for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, z[k][r]);
+  mx = over_halves(mx, [](float x, float y) { return fmaxf(x, y); }) * scale2;
+  if (__any(mx > run.top)) {
+    const float now = fmaxf(run.top, mx);
+    const float keep = __builtin_amdgcn_exp2f(run.top - (now == -INFINITY ? 0.0f : now));
+    run.sum *= keep;
+#pragma unroll
+    for (int t = 0; t < DTILES; ++t) acc[t] *= keep;
+    run.top = now;
+  }
+  const float ref = run.top == -INFINITY ? 0.0f : run.top;
+  float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // the block's own sum first: a long list has thousands of blocks
+#pragma unroll
+  for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float seen = CAREFUL && z[k][r] != -INFINITY ? 1.0f : 0.0f;
+      z[k][r] = __builtin_amdgcn_exp2f(fmaf(z[k][r], scale2, -ref));
+      part[r % 4] += z[k][r];
+      if (CAREFUL && mode != kFinite) z[k][r] = seen;
+    }
+  run.sum += (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+// Whether a sweep has left something that is not finite, and what the sweeps over V's marks say of it.
+template <int DTILES>
+__device__ __forceinline__ bool not_finite(const f32x16_p (&acc)[DTILES]) {
+  bool any = false;
+#pragma unroll
+  for (int t = 0; t < DTILES; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) any |= !(fabsf(acc[t][r]) < INFINITY);
+  return any;
+}
+struct Marks {
+  uint64_t up = 0, down = 0;  // bit 16 t + r
+};
+template <int DTILES>
+__device__ __forceinline__ void take_marks(Marks &marks, f32x16_p (&acc)[DTILES], int mode) {
+#pragma unroll
+  for (int t = 0; t < DTILES; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const uint64_t bit = 1ull << (16 * t + r);
+      if (mode == kUp) marks.up |= acc[t][r] > 0.0f ? bit : 0;
+      else if (mode == kDown) marks.down |= acc[t][r] > 0.0f ? bit : 0;
+      else if ((marks.up | marks.down) & bit) acc[t][r] += !(marks.up & bit) ? -INFINITY : !(marks.down & bit) ? INFINITY : NAN;
+    }
+}
+
+// Partial sums joined: what is infinite or NaN weighs in, however little its part weighs.
+__device__ __forceinline__ f32x4_p add_part(f32x4_p num, const f32x4_p &x, float f) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) num[e] = fabsf(x[e]) < INFINITY ? fmaf(x[e], f, num[e]) : num[e] + x[e];
+  return num;
+}
+
+// Four components of an output row.
+template <int DT>
+__device__ __forceinline__ void store_out(char *row, int d, const f32x4_p &x) {
+  if (DT == CKV_BF16) *reinterpret_cast<uint2 *>(row + 2 * d) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+  else *reinterpret_cast<f32x4_p *>(row + 4 * d) = x;
+}
+__device__ __forceinline__ char *out_row(const PagedArgs &a, int b, const Column &c) {
+  return a.out + b * a.os[0] + c.h * a.os[1] + c.token * a.os[2];
+}
+__device__ __forceinline__ float inverse_sum(float sum) { return sum == 0.0f ? 0.0f : 1.0f / sum; }
+__device__ __forceinline__ void store_lse(const PagedArgs &a, int b, const Column &c, float top, float sum) {
+  if (a.lse) a.lse[((size_t)b * a.Hq + c.h) * a.n + c.token] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+}
+
+constexpr int kRowsCols = 32;  // columns of a tile of paged_rows_kernel
+void launch_paged_rows(const PagedArgs &a, bool bf16, int d, hipStream_t stream);
+
+}  // namespace ckv
+#endif

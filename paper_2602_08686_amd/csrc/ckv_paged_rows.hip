@@ -1,0 +1,184 @@
+// Attention over pages for few columns (decoding steps, drafted tokens): bound by memory, every row once.
+//
+// All of a tile's columns are one operand of the matrix products (32 of them, however many exist), and the workgroup's waves
+// share out the rows, 32 at a time, each with a place in LDS of its own for them: no barrier between the first row and the last. A wave's
+// loads go straight to LDS. K's place is free once the first product has read it and V's once the second has, so the next
+// 32 rows' K is on its way during the softmax and the second product, their V during the next first product. Page numbers
+// come the same way, one block further ahead; a lane per row turns them into offsets.
+// Waves are joined in LDS in wave order, chunks by paged_merge_kernel in chunk order.
+#include "ckv_paged.h"
+
+namespace ckv {
+
+template <int DT, int DH, int WAVES, bool STREAM>
+__global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(PagedArgs a) {
+  typedef Image<DT, DH> I;
+  constexpr int LOADS = 32 / I::ROWS_PER_LOAD;  // of K, and of V, per block
+  constexpr int BLOCK = 32 * I::ROW;
+  constexpr int PIECES = DH / 4;                // of 16 bytes of a column's fp32 sums
+  __shared__ __align__(1024) char s_rows[WAVES][2][BLOCK];
+  __shared__ __align__(256) int32_t s_ids[WAVES][2][kWave];
+  struct Offsets {
+    int64_t k, v;
+  };
+  __shared__ Offsets s_at[WAVES][32];
+  __shared__ float2 s_stats[WAVES][32];
+  static_assert(32 * DH * 4 <= 2 * BLOCK, "a wave's sums take its rows' place");
+
+  int at = work_item(blockIdx.x, a.workgroups);
+  const int chunk = at % a.n_chunks;
+  at /= a.n_chunks;
+  const int tile = at % a.col_tiles, unit = at / a.col_tiles;
+  const int b = unit / a.Hkv, g = unit % a.Hkv;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 31, half = lane >> 5;
+  const TileRange range = tile_range(a, unit, tile);
+  if (range.cols <= 0) return;
+  const int first = chunk * range.per_chunk, last = min(first + range.per_chunk, range.stages);  // blocks of 32 rows
+  const bool single = a.n_chunks == 1;
+  if (first >= last && !single) return;  // the merge reads the chunks that have blocks
+
+  const bool valid = m < range.cols;
+  const Column c = column(a, unit, tile, valid ? m : 0);
+  const int sees_least = __builtin_amdgcn_readfirstlane(c.limit);
+  u32x4_d qf[I::STEPS];
+  load_query<DT, DH>(a, b, c, valid, half, qf);
+
+  const int32_t *list = a.lists.table + b * a.lists.table_b + g * a.lists.table_h;
+  const char *kb = a.k + g * a.lists.ks[1], *vb = a.v + g * a.lists.vs[1];
+  char *k_rows = s_rows[wave][0], *v_rows = s_rows[wave][1];
+  // Rows behind the end are the last one again; a page that is not in the pool is page 0 (they weigh nothing).
+  auto row_of = [&](int block) { return min(block * 32 + m, range.end - 1); };
+  auto fetch_ids = [&](int block, int slot) { dma_4(list + (row_of(block) >> a.lists.shift), s_ids[wave][slot]); };
+  auto find_rows = [&](int block, int slot) {  // returns which of the 32 are on no page
+    const int id = s_ids[wave][slot][m], row = row_of(block) & ((1 << a.lists.shift) - 1);
+    const bool ok = (unsigned)id < (unsigned)a.lists.n_pages;
+    const int64_t page = ok ? id : 0;
+    if (half == 0) s_at[wave][m] = Offsets{page * a.lists.ks[0] + row * a.lists.ks[2], page * a.lists.vs[0] + row * a.lists.vs[2]};
+    const uint32_t missing = (uint32_t)__ballot(!ok);
+    wait_lds_reads();
+    return missing;
+  };
+  auto fetch_k = [&]() {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int row = j * I::ROWS_PER_LOAD + lane / I::PIECES;
+      dma_16<STREAM>(kb + s_at[wave][row].k + I::k_piece(row, lane % I::PIECES) * 16, k_rows + 1024 * j);
+    }
+  };
+  auto fetch_v = [&]() {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int row = j * I::ROWS_PER_LOAD + lane / I::PIECES;
+      dma_16<STREAM>(vb + s_at[wave][row].v + I::v_piece(row, lane % I::PIECES) * 16, v_rows + 1024 * j);
+    }
+  };
+
+  Running run;
+  f32x16_p acc[I::DTILES];
+  auto sweep = [&](auto careful, int mode) {
+    constexpr bool CAREFUL = decltype(careful)::value;
+    run = Running{-INFINITY, 0.0f};
+#pragma unroll
+    for (int t = 0; t < I::DTILES; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[t][r] = 0.0f;
+    int block = first + wave, slot = 0;
+    if (block >= last) return;
+    fetch_ids(block, 0);
+    fetch_ids(block + WAVES, 1);
+    wait_vm_at_most<1>();
+    uint32_t missing = find_rows(block, 0);
+    fetch_k();
+    fetch_v();
+    for (; block < last; block += WAVES, slot ^= 1) {
+      const bool more = block + WAVES < last;
+      uint32_t next_missing = 0;
+      f32x16_p z[1];
+      wait_vm_at_most<LOADS>();  // K, and the next page numbers; V may be on its way
+      first_product<DT, DH>(k_rows, lane, qf, z[0]);
+      wait_lds_reads();
+      if (more) {
+        next_missing = find_rows(block + WAVES, slot ^ 1);
+        fetch_ids(block + 2 * WAVES, slot);
+        fetch_k();
+      }
+      if (missing || (block + 1) * 32 > sees_least) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = block_row(r, half);
+          if (block * 32 + row >= c.limit || (missing >> row & 1)) z[0][r] = -INFINITY;
+        }
+      }
+      online_softmax<1, I::DTILES, CAREFUL>(z, a.scale2, run, acc, mode);
+      if (more) wait_vm_at_most<LOADS + 1>();  // V; the next page numbers and K may be on their way
+      else wait_vm_at_most<0>();
+      second_product<DT, DH, CAREFUL>(v_rows, lane, z[0], acc, mode);
+      wait_lds_reads();
+      if (more) fetch_v();
+      missing = next_missing;
+    }
+  };
+  sweep(std::false_type{}, kFinite);
+  if (__any(valid && not_finite(acc))) {
+    Marks marks;
+    for (int mode = kUp; mode <= kFinite; ++mode) {
+      sweep(std::true_type{}, mode);
+      take_marks(marks, acc, mode);
+    }
+  }
+  run.sum = over_halves(run.sum, [](float x, float y) { return x + y; });
+
+  // the waves' sums in their rows' places, the pieces of a column permuted by it
+  if (valid) {
+    char *to = s_rows[wave][0] + m * DH * 4;
+#pragma unroll
+    for (int t = 0; t < I::DTILES; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f32x4_p *>(to + (((8 * t + 2 * r + half) ^ m) % PIECES) * 16) =
+            f32x4_p{acc[t][4 * r], acc[t][4 * r + 1], acc[t][4 * r + 2], acc[t][4 * r + 3]};
+    if (half == 0) s_stats[wave][m] = make_float2(run.top, run.sum);
+  }
+  __syncthreads();
+  const size_t row0 = (((size_t)unit * a.col_tiles + tile) * a.n_chunks + chunk) * kRowsCols;
+  for (int i = threadIdx.x; i < range.cols * PIECES; i += WAVES * kWave) {
+    const int local = i / PIECES, piece = i % PIECES;
+    float top = s_stats[0][local].x, sum = 0.0f;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_stats[w][local].x);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    f32x4_p num = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float2 st = s_stats[w][local];
+      const float f = __builtin_amdgcn_exp2f(st.x - ref);
+      sum = fmaf(st.y, f, sum);
+      num = add_part(num, *reinterpret_cast<const f32x4_p *>(s_rows[w][0] + local * DH * 4 + ((piece ^ local) % PIECES) * 16), f);
+    }
+    if (single) {
+      const Column o = column(a, unit, tile, local);
+      store_out<DT>(out_row(a, b, o), 4 * piece, num * inverse_sum(sum));
+      if (piece == 0) store_lse(a, b, o, top, sum);
+    } else {
+      *reinterpret_cast<f32x4_p *>(a.part + (row0 + local) * DH + 4 * piece) = num;
+      if (piece == 0) a.stats[row0 + local] = make_float2(top, sum);
+    }
+  }
+}
+
+template <int DT, int DH, int WAVES>
+static void launch_rows_attention(const PagedArgs &a, hipStream_t stream) {
+  // rows that one workgroup only reads are used once
+  if (a.col_tiles == 1) hipLaunchKernelGGL((paged_rows_kernel<DT, DH, WAVES, true>), dim3((unsigned)a.workgroups), dim3(WAVES * kWave), 0, stream, a);
+  else hipLaunchKernelGGL((paged_rows_kernel<DT, DH, WAVES, false>), dim3((unsigned)a.workgroups), dim3(WAVES * kWave), 0, stream, a);
+}
+
+// As many waves as have a place for 32 rows of K and of V each, eight at most.
+void launch_paged_rows(const PagedArgs &a, bool bf16, int d, hipStream_t stream) {
+  if (bf16 && d == 128) launch_rows_attention<CKV_BF16, 128, 8>(a, stream);
+  else if (bf16) launch_rows_attention<CKV_BF16, 64, 8>(a, stream);
+  else if (d == 128) launch_rows_attention<CKV_F32, 128, 4>(a, stream);
+  else launch_rows_attention<CKV_F32, 64, 8>(a, stream);
+}
+
+}  // namespace ckv

@@ -38,8 +38,10 @@ hipError_t launch_rows(const ckv_params *p, const Shape &s, const ckv_rotation *
 
 // Attention over the pages: how a call is shared out, from sizes alone.
 struct PagedPlan {
+  bool by_rows;      // paged_rows_kernel: few columns, a workgroup's waves share out the rows
   int tile_cols;     // query columns (heads of a group times new tokens) of a workgroup
   int col_tiles;     // such tiles of a (batch element, KV head)
+  int stage_rows;    // rows of a list are shared out in multiples of this
   int n_chunks;      // workgroups along the rows of a list
   int64_t workgroups;
   size_t workspace_bytes;

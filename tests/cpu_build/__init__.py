@@ -22,7 +22,7 @@ def build(where) -> str:
     objs, procs = [], []
     csrc = ROOT / "paper_2602_08686_amd" / "csrc"
     for src in (csrc / "ckv_api.hip", csrc / "ckv_select.hip", csrc / "ckv_decode.hip", csrc / "ckv_gather.hip", csrc / "ckv_rows.hip", csrc / "ckv_paged.hip",
-                HERE / "emulator.cpp"):
+                csrc / "ckv_paged_rows.hip", HERE / "emulator.cpp"):
         objs.append(str(pathlib.Path(where) / (src.name + ".o")))
         procs.append(subprocess.Popen([CXX, "-x", "c++", "-std=c++17", "-O1", "-fPIC", "-w", "-fsanitize=bounds", "-fsanitize-trap=bounds",
                                        f"-I{HERE}", f"-I{ROOT / 'include'}", f"-I{csrc}", "-c", str(src), "-o", objs[-1]]))

@@ -142,9 +142,6 @@ template <class P> auto read_tr16(P at) {  // P: a pointer to four words in LDS
   return out;
 }
 #define __builtin_amdgcn_ds_read_tr16_b64_v4i16(at) read_tr16(at)
-// There at once: what the wait is for does not show here.
-#define __builtin_amdgcn_global_load_lds(from, lds, bytes, offset, aux) memcpy((char *)(lds) + (bytes) * emu::lane(), (const void *)(from), bytes)
-#define __builtin_amdgcn_s_waitcnt(x) ((void)0)
 inline void sincospif(float x, float *s, float *c) {
   *s = (float)sin(3.14159265358979323846 * (double)x);
   *c = (float)cos(3.14159265358979323846 * (double)x);
