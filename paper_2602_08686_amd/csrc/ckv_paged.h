@@ -122,15 +122,23 @@ __device__ __forceinline__ void mma_piece(f32x16_p &acc, const u32x4_d &x, const
 
 // First product of 32 rows of K: element r is the product of row block_row(r, half) with the lane's column (lane % 32).
 __device__ __forceinline__ int block_row(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
+// Bytes from an image of K to the lane's piece 0, and piece 2 s + half of its row: the permutation is an exclusive or of the piece's
+// number, so a step is one of the address (images start at multiples of a row).
+template <int DT, int DH>
+__device__ __forceinline__ int k_lane(int lane) {
+  typedef Image<DT, DH> I;
+  return (lane & 31) * I::ROW + I::k_piece(lane & 31, lane >> 5) * 16;
+}
+__device__ __forceinline__ u32x4_d k_operand(const char *image, int at, int s) {
+  return *reinterpret_cast<const u32x4_d *>(image + (at ^ (32 * s)));
+}
 template <int DT, int DH>
 __device__ __forceinline__ void first_product(const char *image, int lane, const u32x4_d (&qf)[Image<DT, DH>::STEPS], f32x16_p &z) {
-  typedef Image<DT, DH> I;
-  const int row = lane & 31, half = lane >> 5;
+  const int at = k_lane<DT, DH>(lane);
 #pragma unroll
   for (int r = 0; r < 16; ++r) z[r] = 0.0f;
 #pragma unroll
-  for (int s = 0; s < I::STEPS; ++s)
-    mma_piece<DT>(z, *reinterpret_cast<const u32x4_d *>(image + row * I::ROW + I::k_piece(row, 2 * s + half) * 16), qf[s]);
+  for (int s = 0; s < Image<DT, DH>::STEPS; ++s) mma_piece<DT>(z, k_operand(image, at, s), qf[s]);
 }
 
 // How a second sweep takes V's components: ones where there is an infinity of one sign or a NaN, or the finite ones only.
@@ -153,46 +161,74 @@ __device__ __forceinline__ uint32_t v_word(uint32_t x, int mode) {
   return mode == kFinite ? (finite ? x : 0u) : (marked ? 0x3f800000u : 0u);
 }
 
-// Second product of 32 rows of V with the weights w (as the first product left the logits): component 32 t + block_row(r, half) of the lane's
-// column is acc[t][r]. CAREFUL: V's components as `mode` says. In bf16 the weights are rounded to the type, to the nearest: 2^-9 of each on
-// average, of both signs, which over many rows is less than the output's own rounding.
-template <int DT, int DH, bool CAREFUL>
-__device__ __forceinline__ void second_product(const char *image, int lane, const f32x16_p &w, f32x16_p (&acc)[DH / 32], int mode) {
-  typedef Image<DT, DH> I;
-  const int half = lane >> 5;
+// Weights of a block as the second product takes them: in bf16 rounded to the type, to the nearest: 2^-9 of each on average, of both signs, which
+// over many rows is less than the output's own rounding.
+template <int DT>
+struct Weights {
+  u32x4_d piece[DT == CKV_BF16 ? 2 : 4];
+};
+template <int DT>
+__device__ __forceinline__ Weights<DT> as_operand(const f32x16_p &w) {
+  Weights<DT> out;
   if constexpr (DT == CKV_BF16) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      u32x4_d y;  // weights of rows 16 j + 4 half + (0..3), and of those eight further on
+    for (int e = 0; e < 8; ++e) out.piece[e / 4][e % 4] = pack_bf16(w[2 * e], w[2 * e + 1]);
+  } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = pack_bf16(w[8 * j + 2 * e], w[8 * j + 2 * e + 1]);
+    for (int e = 0; e < 16; ++e) out.piece[e / 4][e % 4] = __float_as_uint(w[e]);
+  }
+  return out;
+}
+
+// The values are computed where this stands.
+template <int DT>
+__device__ __forceinline__ void pin(Weights<DT> &w, float &sum) {
+#pragma unroll
+  for (u32x4_d &piece : w.piece) asm volatile("" : "+v"(piece));
+  asm volatile("" : "+v"(sum));
+}
+
+// V's operand in bf16, rows 16 j + 4 half + (0..3) and those eight further on, components 32 t + lane % 32: 16 lanes read four rows of 16
+// components and get a component's four rows each. v_lane: the lane's bytes for t = 0, j = 0.
+template <int DH>
+__device__ __forceinline__ int v_lane(int lane) {
+  typedef Image<CKV_BF16, DH> I;
+  const int row = 4 * (lane >> 5) + (lane & 15) / 4, byte = 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+  return row * I::ROW + I::v_piece(row, byte / 16) * 16 + byte % 16;
+}
+template <int DH>
+__device__ __forceinline__ u32x4_d v_operand(const char *image, int at, int t, int j) {
+  constexpr int ROW = Image<CKV_BF16, DH>::ROW;
+  const char *from = image + (at ^ (64 * t)) + 16 * j * ROW;
+  const u32x2_p lo = read_transposed(from), hi = read_transposed(from + 8 * ROW);
+  return u32x4_d{lo[0], lo[1], hi[0], hi[1]};
+}
+// Second product of 32 rows of V: component 32 t + block_row(r, half) of the lane's column is acc[t][r]. CAREFUL: V's components as `mode` says.
+template <int DT, int DH, bool CAREFUL>
+__device__ __forceinline__ void second_product(const char *image, int lane, const Weights<DT> &w, f32x16_p (&acc)[DH / 32], int mode) {
+  typedef Image<DT, DH> I;
+  if constexpr (DT == CKV_BF16) {
+    const int at = v_lane<DH>(lane);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
 #pragma unroll
       for (int t = 0; t < I::DTILES; ++t) {
-        u32x4_d x;
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          // 16 lanes read four rows of 16 components and get a component's four rows each
-          const int row = 16 * j + 8 * p + 4 * half + (lane & 15) / 4;
-          const int byte = 64 * t + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
-          const u32x2_p two = read_transposed(image + row * I::ROW + I::v_piece(row, byte / 16) * 16 + byte % 16);
-          x[2 * p] = two[0];
-          x[2 * p + 1] = two[1];
-        }
+        u32x4_d x = v_operand<DH>(image, at, t, j);
         if (CAREFUL)
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[e] = v_word<DT>(x[e], mode);
-        mma_piece<DT>(acc[t], x, y);
+        mma_piece<DT>(acc[t], x, w.piece[j]);
       }
     }
   } else {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int row = block_row(r, half);
+      const int row = block_row(r, lane >> 5);
 #pragma unroll
       for (int t = 0; t < I::DTILES; ++t) {
         uint32_t x = *reinterpret_cast<const uint32_t *>(image + row * I::ROW + (32 * t + (lane & 31)) * 4);
         if (CAREFUL) x = v_word<DT>(x, mode);
-        acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x), w[r], acc[t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x), __uint_as_float(w.piece[r / 4][r % 4]), acc[t], 0, 0, 0);
       }
     }
   }
@@ -202,35 +238,45 @@ __device__ __forceinline__ void second_product(const char *image, int lane, cons
 struct Running {
   float top, sum;
 };
-// Logits to weights. A new maximum scales what there is: rare after the first blocks. CAREFUL with a mode other than kFinite: the weights become ones.
-template <int BLOCKS, int DTILES, bool CAREFUL>
-__device__ __forceinline__ void online_softmax(f32x16_p (&z)[BLOCKS], float scale2, Running &run, f32x16_p (&acc)[DTILES], int mode) {
-  float mx = z[0][0];
-#pragma unroll
-  for (int k = 0; k < BLOCKS; ++k)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, z[k][r]);
+// Logits of a block to weights; returns what the sums of V so far are to be multiplied by. The reference moves only where the maximum
+// outgrows it by kSlack (weights up to 2^kSlack: fp32 and bf16 keep their relative precision), which it hardly ever does behind the
+// first blocks. CAREFUL with a mode other than kFinite: the weights become ones.
+constexpr float kSlack = 6.0f;
+// ... from the maximum of this half's rows (of the products, not yet scaled)
+__device__ __forceinline__ float new_reference(float mx, float scale2, Running &run, float *ref) {
   mx = over_halves(mx, [](float x, float y) { return fmaxf(x, y); }) * scale2;
-  if (__any(mx > run.top)) {
-    const float now = fmaxf(run.top, mx);
-    const float keep = __builtin_amdgcn_exp2f(run.top - (now == -INFINITY ? 0.0f : now));
-    run.sum *= keep;
+  const float now = mx > run.top + kSlack ? mx : run.top;
+  *ref = now == -INFINITY ? 0.0f : now;
+  const float keep = now == run.top ? 1.0f : __builtin_amdgcn_exp2f(run.top - *ref);
+  run.top = now;
+  return keep;
+}
+template <bool CAREFUL>
+__device__ __forceinline__ float to_weights(f32x16_p &z, float scale2, Running &run, int mode) {
+  float mx = z[0], ref;
+#pragma unroll
+  for (int r = 1; r < 16; ++r) mx = fmaxf(mx, z[r]);
+  const float keep = new_reference(mx, scale2, run, &ref);
+  float part[4];  // the block's own sum first: a long list has thousands of blocks
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const float seen = CAREFUL && z[r] != -INFINITY ? 1.0f : 0.0f;
+    z[r] = __builtin_amdgcn_exp2f(fmaf(z[r], scale2, -ref));
+    part[r % 4] = r < 4 ? z[r] : part[r % 4] + z[r];
+    if (CAREFUL && mode != kFinite) z[r] = seen;
+  }
+  run.sum = fmaf(run.sum, keep, (part[0] + part[1]) + (part[2] + part[3]));
+  return keep;
+}
+
+// The sums so far times `keep`. A branch that stays one: without the statement in it the products are made every time.
+template <int DTILES>
+__device__ __forceinline__ void rescale(f32x16_p (&acc)[DTILES], float keep) {
+  if (__any(keep != 1.0f)) {
+    asm volatile("" ::: "memory");
 #pragma unroll
     for (int t = 0; t < DTILES; ++t) acc[t] *= keep;
-    run.top = now;
   }
-  const float ref = run.top == -INFINITY ? 0.0f : run.top;
-  float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // the block's own sum first: a long list has thousands of blocks
-#pragma unroll
-  for (int k = 0; k < BLOCKS; ++k)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float seen = CAREFUL && z[k][r] != -INFINITY ? 1.0f : 0.0f;
-      z[k][r] = __builtin_amdgcn_exp2f(fmaf(z[k][r], scale2, -ref));
-      part[r % 4] += z[k][r];
-      if (CAREFUL && mode != kFinite) z[k][r] = seen;
-    }
-  run.sum += (part[0] + part[1]) + (part[2] + part[3]);
 }
 
 // Whether a sweep has left something that is not finite, and what the sweeps over V's marks say of it.

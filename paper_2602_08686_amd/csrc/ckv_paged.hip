@@ -17,16 +17,74 @@
 namespace ckv {
 
 constexpr int kTileWaves = 4;
-constexpr int tile_stage_rows(bool bf16) { return bf16 ? 64 : 32; }
+constexpr int kStageRows = 64;  // two blocks of 32 rows
+
+// A whole step in bf16, its instructions in the order that they are issued in: slot by slot a matrix product (the two kinds in turn), the operands
+// of those two or four slots further on, and a share of the softmax: first the maximum, then a few exponentials each. Left to itself the compiler puts
+// all products first, each behind a wait for its operand. `next` gets the logits of K's block, `weights` changes from the block before to z's.
+template <int DT, int DH>
+__device__ __forceinline__ float whole_step(const char *k_image, const char *v_image, int lane, const u32x4_d (&qf)[Image<DT, DH>::STEPS],
+                                            const f32x16_p &z, f32x16_p &next, Weights<DT> &weights, f32x16_p (&acc)[DH / 32], float scale2, Running &run) {
+  constexpr int STEPS = DH / 16, DTILES = DH / 32, SLOTS = 2 * STEPS, MAX_SLOTS = SLOTS / 4, EXP_SLOTS = SLOTS - MAX_SLOTS;
+  static_assert(DT == CKV_BF16 && 2 * DTILES == STEPS, "as many products of one kind as of the other");
+  constexpr int AHEAD = 2;
+  const int k_at = k_lane<CKV_BF16, DH>(lane), v_at = v_lane<DH>(lane);
+  u32x4_d kf[STEPS], vf[STEPS];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    kf[i] = k_operand(k_image, k_at, i);
+    vf[i] = v_operand<DH>(v_image, v_at, i % DTILES, i / DTILES);
+  }
+  float mx = z[0], ref = 0.0f, keep = 1.0f, part[4], w[16];
+  Weights<DT> made;
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int slot = 0; slot < SLOTS; ++slot) {
+    const int i = slot / 2;
+    if (slot % 2 == 0) {
+      if (i + AHEAD < STEPS) kf[i + AHEAD] = k_operand(k_image, k_at, i + AHEAD);
+      if (i == 0) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) next[r] = 0.0f;
+      }
+      mma_piece<CKV_BF16>(next, kf[i], qf[i]);
+    } else {
+      if (i + AHEAD < STEPS) vf[i + AHEAD] = v_operand<DH>(v_image, v_at, (i + AHEAD) % DTILES, (i + AHEAD) / DTILES);
+      mma_piece<CKV_BF16>(acc[i % DTILES], vf[i], weights.piece[i / DTILES]);
+    }
+    if (slot < MAX_SLOTS) {
+#pragma unroll
+      for (int r = slot * 16 / MAX_SLOTS; r < (slot + 1) * 16 / MAX_SLOTS; ++r) mx = fmaxf(mx, z[r]);
+      if (slot == MAX_SLOTS - 1) keep = new_reference(mx, scale2, run, &ref);
+    } else {
+#pragma unroll
+      for (int r = (slot - MAX_SLOTS) * 16 / EXP_SLOTS; r < (slot - MAX_SLOTS + 1) * 16 / EXP_SLOTS; ++r) {
+        w[r] = __builtin_amdgcn_exp2f(fmaf(z[r], scale2, -ref));
+        part[r % 4] = r < 4 ? w[r] : part[r % 4] + w[r];
+        if (r % 2) made.piece[r / 8][r / 2 % 4] = pack_bf16(w[r - 1], w[r]);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  run.sum = fmaf(run.sum, keep, (part[0] + part[1]) + (part[2] + part[3]));
+  weights = made;
+  return keep;
+}
 
 template <int DT, int DH, int WAVES>
-__global__ void __launch_bounds__(WAVES *kWave, 2) paged_tile_kernel(PagedArgs a) {
+__global__ void __launch_bounds__(WAVES *kWave, DH * (DT == CKV_BF16 ? 2 : 4) > 256 ? 1 : 2) paged_tile_kernel(PagedArgs a) {
   typedef Image<DT, DH> I;
-  constexpr int ROWS = tile_stage_rows(DT == CKV_BF16), BLOCKS = ROWS / 32, BYTES = ROWS * I::ROW;
-  constexpr int LOADS = BYTES / 1024 / WAVES;  // of K per wave and stage, and of V
-  static_assert(LOADS * WAVES * 1024 == BYTES, "whole loads");
+  constexpr int BYTES = kStageRows * I::ROW;
+  constexpr int LOADS = BYTES / 1024 / WAVES;       // of K per wave and stage, and of V
+  constexpr int OWN = LOADS * I::ROWS_PER_LOAD;     // rows that a wave fetches
+  static_assert(OWN * WAVES == kStageRows && OWN <= kWave, "whole loads");
   __shared__ __align__(1024) char s_k[2][BYTES];
   __shared__ __align__(1024) char s_v[2][BYTES];
+  __shared__ __align__(256) int32_t s_ids[WAVES][kWave];
+  struct Offsets {
+    int64_t k, v;
+  };
+  __shared__ Offsets s_at[WAVES][2][OWN];
   __shared__ int s_missing, s_undefined;
 
   int at = work_item(blockIdx.x, a.workgroups);
@@ -44,9 +102,7 @@ __global__ void __launch_bounds__(WAVES *kWave, 2) paged_tile_kernel(PagedArgs a
   const int local = wave * 32 + (lane & 31);
   const bool valid = local < range.cols;
   const Column c = column(a, unit, tile, valid ? local : 0);
-  // of the wave: its first column sees the fewest rows, the last that exists the most
-  const int sees_least = __builtin_amdgcn_readfirstlane(c.limit);
-  const int sees_most = wave * 32 < range.cols ? column(a, unit, tile, min(range.cols, wave * 32 + 32) - 1).limit : 0;
+  const int sees_least = __builtin_amdgcn_readfirstlane(c.limit);  // the wave's first column sees the fewest rows
   u32x4_d qf[I::STEPS];
   load_query<DT, DH>(a, b, c, valid, half, qf);
 
@@ -55,67 +111,151 @@ __global__ void __launch_bounds__(WAVES *kWave, 2) paged_tile_kernel(PagedArgs a
   if (threadIdx.x == 0) s_missing = s_undefined = 0;
   __syncthreads();
 
-  // Rows behind the end are the last one again; a page that is not in the pool is page 0 (they weigh nothing).
-  auto fetch = [&](int stage, int buf) {
+  // A wave's own rows of a stage: page numbers, then offsets, then the rows. Rows behind the end are the last one again; a page that is
+  // not in the pool is page 0 (they weigh nothing).
+  auto own_row = [&](int stage) { return min(stage * kStageRows + wave * OWN + lane % OWN, range.end - 1); };
+  auto fetch_ids = [&](int stage) { dma_4(list + (own_row(stage) >> a.lists.shift), s_ids[wave]); };
+  auto find_rows = [&](int stage) {
+    const int id = s_ids[wave][lane], row = own_row(stage) & ((1 << a.lists.shift) - 1);
+    const bool ok = (unsigned)id < (unsigned)a.lists.n_pages;
+    const int64_t page = ok ? id : 0;
+    if (!ok) s_missing = 1;
+    if (lane < OWN) s_at[wave][stage & 1][lane] = Offsets{page * a.lists.ks[0] + row * a.lists.ks[2], page * a.lists.vs[0] + row * a.lists.vs[2]};
+    wait_lds_reads();
+  };
+  auto fetch_k = [&](int stage) {
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int block = wave * LOADS + j, row = block * I::ROWS_PER_LOAD + lane / I::PIECES, piece = lane % I::PIECES;
-      const int at_row = min(stage * ROWS + row, range.end - 1);
-      int page = list[at_row >> a.lists.shift];
-      if ((unsigned)page >= (unsigned)a.lists.n_pages) {
-        page = 0;
-        s_missing = 1;
-      }
-      const int64_t r = at_row & ((1 << a.lists.shift) - 1);
-      dma_16<false>(kb + page * a.lists.ks[0] + r * a.lists.ks[2] + I::k_piece(row, piece) * 16, s_k[buf] + block * 1024);
-      dma_16<false>(vb + page * a.lists.vs[0] + r * a.lists.vs[2] + I::v_piece(row, piece) * 16, s_v[buf] + block * 1024);
+      const int own = j * I::ROWS_PER_LOAD + lane / I::PIECES;
+      dma_16<false>(kb + s_at[wave][stage & 1][own].k + I::k_piece(wave * OWN + own, lane % I::PIECES) * 16, s_k[stage & 1] + (wave * LOADS + j) * 1024);
+    }
+  };
+  auto fetch_v = [&](int stage) {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int own = j * I::ROWS_PER_LOAD + lane / I::PIECES;
+      dma_16<false>(vb + s_at[wave][stage & 1][own].v + I::v_piece(wave * OWN + own, lane % I::PIECES) * 16, s_v[stage & 1] + (wave * LOADS + j) * 1024);
     }
   };
 
   Running run;
   f32x16_p acc[I::DTILES];
-  auto sweep = [&](auto careful, int mode) {
-    constexpr bool CAREFUL = decltype(careful)::value;
+  auto begin = [&]() {
     run = Running{-INFINITY, 0.0f};
 #pragma unroll
     for (int t = 0; t < I::DTILES; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[t][r] = 0.0f;
-    if (first < last) fetch(first, 0);
-    for (int stage = first; stage < last; ++stage) {
-      const int buf = (stage - first) & 1, base = stage * ROWS;
-      wait_vm_at_most<0>();
-      __syncthreads();  // the stage is there, and the other buffer has been read
-      if (stage + 1 < last) fetch(stage + 1, buf ^ 1);
-      if (base >= sees_most) continue;
-      const bool missing = s_missing;
-      f32x16_p z[BLOCKS];
-#pragma unroll
-      for (int k = 0; k < BLOCKS; ++k) first_product<DT, DH>(s_k[buf] + 32 * k * I::ROW, lane, qf, z[k]);
-      if (missing || base + ROWS > sees_least) {
-#pragma unroll
-        for (int k = 0; k < BLOCKS; ++k)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int row = base + 32 * k + block_row(r, half);
-            bool seen = row < c.limit;
-            if (missing && seen) seen = (unsigned)list[row >> a.lists.shift] < (unsigned)a.lists.n_pages;
-            if (!seen) z[k][r] = -INFINITY;
-          }
-      }
-      online_softmax<BLOCKS, I::DTILES, CAREFUL>(z, a.scale2, run, acc, mode);
-#pragma unroll
-      for (int k = 0; k < BLOCKS; ++k) second_product<DT, DH, CAREFUL>(s_v[buf] + 32 * k * I::ROW, lane, z[k], acc, mode);
-    }
+    if (first >= last) return false;
+    fetch_ids(first);
+    wait_vm_at_most<0>();
+    find_rows(first);
+    return true;
   };
-  sweep(std::false_type{}, kFinite);
+  // logits of rows that the column does not see
+  auto hide = [&](f32x16_p &z, int z_row) {
+    if (!s_missing && z_row + 32 <= sees_least) return;
+    const int sees = c.limit - z_row - 4 * half;  // rows of the block from the half's first one on
+    uint32_t there = ~0u;
+    if (s_missing) {
+      there = 0;
+#pragma unroll 1
+      for (int r = 0; r < 16; ++r) {
+        const int row = min(z_row + block_row(r, half), range.end - 1);
+        there |= ((unsigned)list[row >> a.lists.shift] < (unsigned)a.lists.n_pages ? 1u : 0u) << r;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (block_row(r, 0) >= sees || !(there >> r & 1)) z[r] = -INFINITY;
+  };
+  constexpr int HALF = 32 * I::ROW;
+
+  if (begin()) {
+    fetch_ids(min(first + 1, last - 1));
+    fetch_k(first);
+    f32x16_p z;           // logits of the block in work
+    Weights<DT> weights;  // of the one before, and what the sums are to be multiplied by before they take them in
+    float keep = 1.0f;
+    // Steps of the pipeline: the first product of a block, the softmax of the one before, the second product of the one before that, none
+    // of which waits for another: the matrix cores have work while the vector units are at the softmax. What is a branch comes in
+    // front, so that the rest is one block of instructions to be scheduled.
+    auto softmax = [&]() {
+      keep = to_weights<false>(z, a.scale2, run, kFinite);
+      weights = as_operand<DT>(z);
+    };
+    auto step = [&](const char *k_image, int z_row, const char *v_image) {
+      rescale(acc, keep);
+      hide(z, z_row);
+      f32x16_p next;
+      if constexpr (DT == CKV_BF16) {
+        keep = whole_step<DT, DH>(k_image, v_image, lane, qf, z, next, weights, acc, a.scale2, run);
+      } else {
+        first_product<DT, DH>(k_image, lane, qf, next);
+        second_product<DT, DH, false>(v_image, lane, weights, acc, kFinite);
+        softmax();
+      }
+      pin(weights, run.sum);  // or the exponentials move behind the next step's branch, away from these products
+      z = next;
+    };
+    auto advance = [&](int stage) {
+      wait_vm_at_most<0>();
+      __syncthreads();  // K of this stage and V of the one before are there, and the buffers of the next loads have been read
+      if (stage + 1 < last) find_rows(stage + 1);
+      if (stage < last) fetch_v(stage);
+      if (stage + 1 < last) {
+        fetch_ids(min(stage + 2, last - 1));
+        fetch_k(stage + 1);
+      }
+    };
+    f32x16_p next;
+    advance(first);
+    first_product<DT, DH>(s_k[first & 1], lane, qf, z);
+    hide(z, first * kStageRows);
+    first_product<DT, DH>(s_k[first & 1] + HALF, lane, qf, next);
+    softmax();
+    z = next;
+#pragma unroll 1
+    for (int stage = first + 1; stage < last; ++stage) {
+      advance(stage);
+      const char *k = s_k[stage & 1], *v = s_v[(stage & 1) ^ 1];
+      step(k, stage * kStageRows - 32, v);
+      step(k + HALF, stage * kStageRows, v + HALF);
+    }
+    advance(last);
+    const char *v = s_v[(last & 1) ^ 1];
+    rescale(acc, keep);
+    second_product<DT, DH, false>(v, lane, weights, acc, kFinite);
+    hide(z, last * kStageRows - 32);
+    softmax();
+    rescale(acc, keep);
+    second_product<DT, DH, false>(v + HALF, lane, weights, acc, kFinite);
+  }
   if (valid && not_finite(acc)) s_undefined = 1;
   __syncthreads();
-  if (s_undefined) {  // the same for all waves, as there are barriers in the sweeps
+  if (s_undefined) {  // the same for all waves, as there are barriers in the sweeps; one block after the other
     Marks marks;
+#pragma unroll 1
     for (int mode = kUp; mode <= kFinite; ++mode) {
-      __syncthreads();  // the buffers have been read
-      sweep(std::true_type{}, mode);
+      begin();
+#pragma unroll 1
+      for (int stage = first; stage < last; ++stage) {
+        __syncthreads();  // the buffers have been read
+        fetch_k(stage);
+        fetch_v(stage);
+        fetch_ids(min(stage + 1, last - 1));
+        wait_vm_at_most<0>();
+        find_rows(min(stage + 1, last - 1));
+        __syncthreads();
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+          f32x16_p z;
+          first_product<DT, DH>(s_k[stage & 1] + k * HALF, lane, qf, z);
+          hide(z, stage * kStageRows + 32 * k);
+          rescale(acc, to_weights<true>(z, a.scale2, run, mode));
+          second_product<DT, DH, true>(s_v[stage & 1] + k * HALF, lane, as_operand<DT>(z), acc, mode);
+        }
+      }
       take_marks(marks, acc, mode);
     }
   }
@@ -173,11 +313,10 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a)
 // ---------------------------------------------------------------------------------------------
 PagedPlan plan_paged(const Shape &s, int n_rows) {
   PagedPlan p;
-  const bool bf16 = s.esize == 2;
   const int64_t units = (int64_t)s.Bz * s.Hkv, cols = (int64_t)s.G * s.T;
   p.by_rows = cols <= kRowsCols;
   p.tile_cols = p.by_rows ? kRowsCols : kTileWaves * 32;
-  p.stage_rows = p.by_rows ? 32 : tile_stage_rows(bf16);
+  p.stage_rows = p.by_rows ? 32 : kStageRows;
   p.col_tiles = (int)((cols + p.tile_cols - 1) / p.tile_cols);
   const int64_t tiles = units * p.col_tiles;
   int64_t chunks = (p.by_rows ? 1 : 2) * kComputeUnits / tiles, most = (n_rows + (p.by_rows ? 511 : 255)) / (p.by_rows ? 512 : 256);

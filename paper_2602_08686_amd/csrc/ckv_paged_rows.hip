@@ -93,9 +93,9 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
     for (; block < last; block += WAVES, slot ^= 1) {
       const bool more = block + WAVES < last;
       uint32_t next_missing = 0;
-      f32x16_p z[1];
+      f32x16_p z;
       wait_vm_at_most<LOADS>();  // K, and the next page numbers; V may be on its way
-      first_product<DT, DH>(k_rows, lane, qf, z[0]);
+      first_product<DT, DH>(k_rows, lane, qf, z);
       wait_lds_reads();
       if (more) {
         next_missing = find_rows(block + WAVES, slot ^ 1);
@@ -106,13 +106,13 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int row = block_row(r, half);
-          if (block * 32 + row >= c.limit || (missing >> row & 1)) z[0][r] = -INFINITY;
+          if (block * 32 + row >= c.limit || (missing >> row & 1)) z[r] = -INFINITY;
         }
       }
-      online_softmax<1, I::DTILES, CAREFUL>(z, a.scale2, run, acc, mode);
+      rescale(acc, to_weights<CAREFUL>(z, a.scale2, run, mode));
       if (more) wait_vm_at_most<LOADS + 1>();  // V; the next page numbers and K may be on their way
       else wait_vm_at_most<0>();
-      second_product<DT, DH, CAREFUL>(v_rows, lane, z[0], acc, mode);
+      second_product<DT, DH, CAREFUL>(v_rows, lane, as_operand<DT>(z), acc, mode);
       wait_lds_reads();
       if (more) fetch_v();
       missing = next_missing;
