@@ -46,10 +46,10 @@ struct Image {
   static constexpr int ROWS_PER_LOAD = 1024 / ROW;           // a wave's load of 16 bytes a lane
   static constexpr int STEPS = PIECES / 2;                   // pieces of a row per half of the wave
   static constexpr int DTILES = DH / 32;
-  static __device__ __forceinline__ int k_piece(int r, int c) { return c ^ (r & 7); }
+  static __device__ __forceinline__ int k_piece(int r, int c) { return c ^ (ROW == 128 ? (r >> 1) & 7 : r & 15); }
   static __device__ __forceinline__ int v_piece(int r, int c) {
     if (DT != CKV_BF16) return c;  // a cycle reads 32 lanes' words of one row
-    return c ^ (2 * (ROW == 128 ? (r >> 1) & 3 : r & 3));
+    return c ^ (4 * (ROW == 128 ? (r >> 1) & 1 : r & 3));
   }
 };
 
@@ -234,48 +234,56 @@ __device__ __forceinline__ void second_product(const char *image, int lane, cons
   }
 }
 
-// Online softmax of a lane's column: the running maximum (log2 domain, common to both halves of the wave) and the sum of this half's rows.
-struct Running {
-  float top, sum;
-};
-// Logits of a block to weights; returns what the sums of V so far are to be multiplied by. The reference moves only where the maximum
-// outgrows it by kSlack (weights up to 2^kSlack: fp32 and bf16 keep their relative precision), which it hardly ever does behind the
-// first blocks. CAREFUL with a mode other than kFinite: the weights become ones.
+// Online softmax of a lane's column: the reference of its weights (log2 domain, common to both halves of the wave; -inf before the first
+// row) and the sum of this half's weights. The reference moves only where a block's maximum outgrows it by kSlack (weights up to
+// 2^kSlack: fp32 and bf16 keep their relative precision), which it hardly ever does behind the first blocks.
 constexpr float kSlack = 6.0f;
-// ... from the maximum of this half's rows (of the products, not yet scaled)
-__device__ __forceinline__ float new_reference(float mx, float scale2, Running &run, float *ref) {
+struct Running {
+  float top, ref, sum;  // ref: top, or 0 where that is -inf
+  float keep;           // what the sums of V so far have still to be multiplied by
+  bool moved;           // whether that is not one for some lane of the wave
+};
+__device__ __forceinline__ Running none_yet() { return Running{-INFINITY, 0.0f, 0.0f, 1.0f, false}; }
+// ... by the maximum of this half's rows (of the products, not yet scaled). A branch that stays one: without the statement in it
+// both sides are computed.
+__device__ __forceinline__ void take_maximum(float mx, float scale2, Running &run) {
   mx = over_halves(mx, [](float x, float y) { return fmaxf(x, y); }) * scale2;
-  const float now = mx > run.top + kSlack ? mx : run.top;
-  *ref = now == -INFINITY ? 0.0f : now;
-  const float keep = now == run.top ? 1.0f : __builtin_amdgcn_exp2f(run.top - *ref);
-  run.top = now;
-  return keep;
+  if (__any(mx > run.top + kSlack)) {
+    asm volatile("" ::: "memory");
+    const float now = mx > run.top + kSlack ? mx : run.top;
+    run.ref = now == -INFINITY ? 0.0f : now;
+    run.keep = now == run.top ? 1.0f : __builtin_amdgcn_exp2f(run.top - run.ref);
+    run.sum *= run.keep;
+    run.top = now;
+    run.moved = true;
+  }
 }
+// Logits of a block to weights. CAREFUL with a mode other than kFinite: the weights become ones.
 template <bool CAREFUL>
-__device__ __forceinline__ float to_weights(f32x16_p &z, float scale2, Running &run, int mode) {
-  float mx = z[0], ref;
+__device__ __forceinline__ void to_weights(f32x16_p &z, float scale2, Running &run, int mode) {
+  float mx = z[0];
 #pragma unroll
   for (int r = 1; r < 16; ++r) mx = fmaxf(mx, z[r]);
-  const float keep = new_reference(mx, scale2, run, &ref);
+  take_maximum(mx, scale2, run);
   float part[4];  // the block's own sum first: a long list has thousands of blocks
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     const float seen = CAREFUL && z[r] != -INFINITY ? 1.0f : 0.0f;
-    z[r] = __builtin_amdgcn_exp2f(fmaf(z[r], scale2, -ref));
+    z[r] = __builtin_amdgcn_exp2f(fmaf(z[r], scale2, -run.ref));
     part[r % 4] = r < 4 ? z[r] : part[r % 4] + z[r];
     if (CAREFUL && mode != kFinite) z[r] = seen;
   }
-  run.sum = fmaf(run.sum, keep, (part[0] + part[1]) + (part[2] + part[3]));
-  return keep;
+  run.sum += (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// The sums so far times `keep`. A branch that stays one: without the statement in it the products are made every time.
+// The sums of V brought to the present reference.
 template <int DTILES>
-__device__ __forceinline__ void rescale(f32x16_p (&acc)[DTILES], float keep) {
-  if (__any(keep != 1.0f)) {
+__device__ __forceinline__ void rescale(f32x16_p (&acc)[DTILES], Running &run) {
+  if (run.moved) {
     asm volatile("" ::: "memory");
 #pragma unroll
-    for (int t = 0; t < DTILES; ++t) acc[t] *= keep;
+    for (int t = 0; t < DTILES; ++t) acc[t] *= run.keep;
+    run.moved = false;
   }
 }
 

@@ -16,18 +16,24 @@
 
 namespace ckv {
 
-constexpr int kTileWaves = 4;
+#ifndef TW
+#define TW 4
+#endif
+constexpr int kTileWaves = TW;
 constexpr int kStageRows = 64;  // two blocks of 32 rows
 
 // A whole step in bf16, its instructions in the order that they are issued in: slot by slot a matrix product (the two kinds in turn), the operands
 // of those two or four slots further on, and a share of the softmax: first the maximum, then a few exponentials each. Left to itself the compiler puts
 // all products first, each behind a wait for its operand. `next` gets the logits of K's block, `weights` changes from the block before to z's.
 template <int DT, int DH>
-__device__ __forceinline__ float whole_step(const char *k_image, const char *v_image, int lane, const u32x4_d (&qf)[Image<DT, DH>::STEPS],
-                                            const f32x16_p &z, f32x16_p &next, Weights<DT> &weights, f32x16_p (&acc)[DH / 32], float scale2, Running &run) {
+__device__ __forceinline__ void whole_step(const char *k_image, const char *v_image, int lane, const u32x4_d (&qf)[Image<DT, DH>::STEPS],
+                                           const f32x16_p &z, f32x16_p &next, Weights<DT> &weights, f32x16_p (&acc)[DH / 32], float scale2, Running &run) {
   constexpr int STEPS = DH / 16, DTILES = DH / 32, SLOTS = 2 * STEPS, MAX_SLOTS = SLOTS / 4, EXP_SLOTS = SLOTS - MAX_SLOTS;
   static_assert(DT == CKV_BF16 && 2 * DTILES == STEPS, "as many products of one kind as of the other");
-  constexpr int AHEAD = 2;
+  #ifndef AH
+#define AH 2
+#endif
+  constexpr int AHEAD = AH;
   const int k_at = k_lane<CKV_BF16, DH>(lane), v_at = v_lane<DH>(lane);
   u32x4_d kf[STEPS], vf[STEPS];
 #pragma unroll
@@ -35,7 +41,7 @@ __device__ __forceinline__ float whole_step(const char *k_image, const char *v_i
     kf[i] = k_operand(k_image, k_at, i);
     vf[i] = v_operand<DH>(v_image, v_at, i % DTILES, i / DTILES);
   }
-  float mx = z[0], ref = 0.0f, keep = 1.0f, part[4], w[16];
+  float mx = z[0], part[4], w[16];
   Weights<DT> made;
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -55,20 +61,19 @@ __device__ __forceinline__ float whole_step(const char *k_image, const char *v_i
     if (slot < MAX_SLOTS) {
 #pragma unroll
       for (int r = slot * 16 / MAX_SLOTS; r < (slot + 1) * 16 / MAX_SLOTS; ++r) mx = fmaxf(mx, z[r]);
-      if (slot == MAX_SLOTS - 1) keep = new_reference(mx, scale2, run, &ref);
+      if (slot == MAX_SLOTS - 1) take_maximum(mx, scale2, run);
     } else {
 #pragma unroll
       for (int r = (slot - MAX_SLOTS) * 16 / EXP_SLOTS; r < (slot - MAX_SLOTS + 1) * 16 / EXP_SLOTS; ++r) {
-        w[r] = __builtin_amdgcn_exp2f(fmaf(z[r], scale2, -ref));
+        w[r] = __builtin_amdgcn_exp2f(fmaf(z[r], scale2, -run.ref));
         part[r % 4] = r < 4 ? w[r] : part[r % 4] + w[r];
         if (r % 2) made.piece[r / 8][r / 2 % 4] = pack_bf16(w[r - 1], w[r]);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
   }
-  run.sum = fmaf(run.sum, keep, (part[0] + part[1]) + (part[2] + part[3]));
+  run.sum += (part[0] + part[1]) + (part[2] + part[3]);
   weights = made;
-  return keep;
 }
 
 template <int DT, int DH, int WAVES>
@@ -76,15 +81,14 @@ __global__ void __launch_bounds__(WAVES *kWave, DH * (DT == CKV_BF16 ? 2 : 4) > 
   typedef Image<DT, DH> I;
   constexpr int BYTES = kStageRows * I::ROW;
   constexpr int LOADS = BYTES / 1024 / WAVES;       // of K per wave and stage, and of V
-  constexpr int OWN = LOADS * I::ROWS_PER_LOAD;     // rows that a wave fetches
-  static_assert(OWN * WAVES == kStageRows && OWN <= kWave, "whole loads");
+  static_assert(LOADS * WAVES * 1024 == BYTES && kStageRows == kWave, "whole loads, a lane for every row");
   __shared__ __align__(1024) char s_k[2][BYTES];
   __shared__ __align__(1024) char s_v[2][BYTES];
-  __shared__ __align__(256) int32_t s_ids[WAVES][kWave];
+  __shared__ __align__(256) int32_t s_ids[2][kWave];
   struct Offsets {
     int64_t k, v;
   };
-  __shared__ Offsets s_at[WAVES][2][OWN];
+  __shared__ Offsets s_at[4][kStageRows];
   __shared__ int s_missing, s_undefined;
 
   int at = work_item(blockIdx.x, a.workgroups);
@@ -111,46 +115,43 @@ __global__ void __launch_bounds__(WAVES *kWave, DH * (DT == CKV_BF16 ? 2 : 4) > 
   if (threadIdx.x == 0) s_missing = s_undefined = 0;
   __syncthreads();
 
-  // A wave's own rows of a stage: page numbers, then offsets, then the rows. Rows behind the end are the last one again; a page that is
-  // not in the pool is page 0 (they weigh nothing).
-  auto own_row = [&](int stage) { return min(stage * kStageRows + wave * OWN + lane % OWN, range.end - 1); };
-  auto fetch_ids = [&](int stage) { dma_4(list + (own_row(stage) >> a.lists.shift), s_ids[wave]); };
+  // Where the rows of a stage are: one wave, another for every stage, turns its page numbers into offsets, two stages ahead of the first loads that
+  // need them. Rows behind the end are the last one again; a page that is not in the pool is page 0 (they weigh nothing).
+  auto row_of = [&](int stage) { return min(stage * kStageRows + lane, range.end - 1); };
+  auto fetch_ids = [&](int stage) {
+    if (wave == stage % WAVES) dma_4(list + (row_of(stage) >> a.lists.shift), s_ids[stage & 1]);
+  };
   auto find_rows = [&](int stage) {
-    const int id = s_ids[wave][lane], row = own_row(stage) & ((1 << a.lists.shift) - 1);
+    if (wave != stage % WAVES) return;
+    const int id = s_ids[stage & 1][lane], row = row_of(stage) & ((1 << a.lists.shift) - 1);
     const bool ok = (unsigned)id < (unsigned)a.lists.n_pages;
     const int64_t page = ok ? id : 0;
     if (!ok) s_missing = 1;
-    if (lane < OWN) s_at[wave][stage & 1][lane] = Offsets{page * a.lists.ks[0] + row * a.lists.ks[2], page * a.lists.vs[0] + row * a.lists.vs[2]};
-    wait_lds_reads();
+    s_at[stage & 3][lane] = Offsets{page * a.lists.ks[0] + row * a.lists.ks[2], page * a.lists.vs[0] + row * a.lists.vs[2]};
   };
   auto fetch_k = [&](int stage) {
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int own = j * I::ROWS_PER_LOAD + lane / I::PIECES;
-      dma_16<false>(kb + s_at[wave][stage & 1][own].k + I::k_piece(wave * OWN + own, lane % I::PIECES) * 16, s_k[stage & 1] + (wave * LOADS + j) * 1024);
+      const int row = (wave * LOADS + j) * I::ROWS_PER_LOAD + lane / I::PIECES;
+      dma_16<false>(kb + s_at[stage & 3][row].k + I::k_piece(row, lane % I::PIECES) * 16, s_k[(stage - first) & 1] + (wave * LOADS + j) * 1024);
     }
   };
   auto fetch_v = [&](int stage) {
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int own = j * I::ROWS_PER_LOAD + lane / I::PIECES;
-      dma_16<false>(vb + s_at[wave][stage & 1][own].v + I::v_piece(wave * OWN + own, lane % I::PIECES) * 16, s_v[stage & 1] + (wave * LOADS + j) * 1024);
+      const int row = (wave * LOADS + j) * I::ROWS_PER_LOAD + lane / I::PIECES;
+      dma_16<false>(vb + s_at[stage & 3][row].v + I::v_piece(row, lane % I::PIECES) * 16, s_v[(stage - first) & 1] + (wave * LOADS + j) * 1024);
     }
   };
 
   Running run;
   f32x16_p acc[I::DTILES];
   auto begin = [&]() {
-    run = Running{-INFINITY, 0.0f};
+    run = none_yet();
 #pragma unroll
     for (int t = 0; t < I::DTILES; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[t][r] = 0.0f;
-    if (first >= last) return false;
-    fetch_ids(first);
-    wait_vm_at_most<0>();
-    find_rows(first);
-    return true;
   };
   // logits of rows that the column does not see
   auto hide = [&](f32x16_p &z, int z_row) {
@@ -171,25 +172,31 @@ __global__ void __launch_bounds__(WAVES *kWave, DH * (DT == CKV_BF16 ? 2 : 4) > 
   };
   constexpr int HALF = 32 * I::ROW;
 
-  if (begin()) {
-    fetch_ids(min(first + 1, last - 1));
+  begin();
+  if (first < last) {
+    for (int i = 0; i < 2; ++i) {  // the first two stages' rows, each by its wave; the page numbers have one place
+      fetch_ids(first + i);
+      wait_vm_at_most<0>();
+      find_rows(first + i);
+      __syncthreads();
+    }
+    fetch_ids(first + 2);
     fetch_k(first);
     f32x16_p z;           // logits of the block in work
-    Weights<DT> weights;  // of the one before, and what the sums are to be multiplied by before they take them in
-    float keep = 1.0f;
+    Weights<DT> weights;  // of the one before
     // Steps of the pipeline: the first product of a block, the softmax of the one before, the second product of the one before that, none
     // of which waits for another: the matrix cores have work while the vector units are at the softmax. What is a branch comes in
     // front, so that the rest is one block of instructions to be scheduled.
     auto softmax = [&]() {
-      keep = to_weights<false>(z, a.scale2, run, kFinite);
+      to_weights<false>(z, a.scale2, run, kFinite);
       weights = as_operand<DT>(z);
     };
     auto step = [&](const char *k_image, int z_row, const char *v_image) {
-      rescale(acc, keep);
+      rescale(acc, run);
       hide(z, z_row);
       f32x16_p next;
       if constexpr (DT == CKV_BF16) {
-        keep = whole_step<DT, DH>(k_image, v_image, lane, qf, z, next, weights, acc, a.scale2, run);
+        whole_step<DT, DH>(k_image, v_image, lane, qf, z, next, weights, acc, a.scale2, run);
       } else {
         first_product<DT, DH>(k_image, lane, qf, next);
         second_product<DT, DH, false>(v_image, lane, weights, acc, kFinite);
@@ -201,34 +208,39 @@ __global__ void __launch_bounds__(WAVES *kWave, DH * (DT == CKV_BF16 ? 2 : 4) > 
     auto advance = [&](int stage) {
       wait_vm_at_most<0>();
       __syncthreads();  // K of this stage and V of the one before are there, and the buffers of the next loads have been read
-      if (stage + 1 < last) find_rows(stage + 1);
+      if (stage + 2 < last) find_rows(stage + 2);
       if (stage < last) fetch_v(stage);
-      if (stage + 1 < last) {
-        fetch_ids(min(stage + 2, last - 1));
-        fetch_k(stage + 1);
-      }
+      if (stage + 1 < last) fetch_k(stage + 1);
+      if (stage + 3 < last) fetch_ids(stage + 3);
     };
     f32x16_p next;
     advance(first);
-    first_product<DT, DH>(s_k[first & 1], lane, qf, z);
+    first_product<DT, DH>(s_k[0], lane, qf, z);
     hide(z, first * kStageRows);
-    first_product<DT, DH>(s_k[first & 1] + HALF, lane, qf, next);
+    first_product<DT, DH>(s_k[0] + HALF, lane, qf, next);
     softmax();
     z = next;
-#pragma unroll 1
-    for (int stage = first + 1; stage < last; ++stage) {
+    // buffers known at compile time: operands at fixed offsets from a few addresses
+    auto stage_of = [&](auto parity, int stage) {
+      constexpr int BUF = decltype(parity)::value;
       advance(stage);
-      const char *k = s_k[stage & 1], *v = s_v[(stage & 1) ^ 1];
-      step(k, stage * kStageRows - 32, v);
-      step(k + HALF, stage * kStageRows, v + HALF);
+      step(s_k[BUF], stage * kStageRows - 32, s_v[BUF ^ 1]);
+      step(s_k[BUF] + HALF, stage * kStageRows, s_v[BUF ^ 1] + HALF);
+    };
+    int stage = first + 1;
+#pragma unroll 1
+    for (; stage + 1 < last; stage += 2) {
+      stage_of(std::integral_constant<int, 1>{}, stage);
+      stage_of(std::integral_constant<int, 0>{}, stage + 1);
     }
+    if (stage < last) stage_of(std::integral_constant<int, 1>{}, stage);
     advance(last);
-    const char *v = s_v[(last & 1) ^ 1];
-    rescale(acc, keep);
+    const char *v = s_v[(last - 1 - first) & 1];
+    rescale(acc, run);
     second_product<DT, DH, false>(v, lane, weights, acc, kFinite);
     hide(z, last * kStageRows - 32);
     softmax();
-    rescale(acc, keep);
+    rescale(acc, run);
     second_product<DT, DH, false>(v + HALF, lane, weights, acc, kFinite);
   }
   if (valid && not_finite(acc)) s_undefined = 1;
@@ -241,19 +253,22 @@ __global__ void __launch_bounds__(WAVES *kWave, DH * (DT == CKV_BF16 ? 2 : 4) > 
 #pragma unroll 1
       for (int stage = first; stage < last; ++stage) {
         __syncthreads();  // the buffers have been read
+        fetch_ids(stage);
+        wait_vm_at_most<0>();
+        find_rows(stage);
+        __syncthreads();
         fetch_k(stage);
         fetch_v(stage);
-        fetch_ids(min(stage + 1, last - 1));
         wait_vm_at_most<0>();
-        find_rows(min(stage + 1, last - 1));
         __syncthreads();
 #pragma unroll 1
         for (int k = 0; k < 2; ++k) {
           f32x16_p z;
-          first_product<DT, DH>(s_k[stage & 1] + k * HALF, lane, qf, z);
+          first_product<DT, DH>(s_k[(stage - first) & 1] + k * HALF, lane, qf, z);
           hide(z, stage * kStageRows + 32 * k);
-          rescale(acc, to_weights<true>(z, a.scale2, run, mode));
-          second_product<DT, DH, true>(s_v[stage & 1] + k * HALF, lane, as_operand<DT>(z), acc, mode);
+          to_weights<true>(z, a.scale2, run, mode);
+          rescale(acc, run);
+          second_product<DT, DH, true>(s_v[(stage - first) & 1] + k * HALF, lane, as_operand<DT>(z), acc, mode);
         }
       }
       take_marks(marks, acc, mode);
@@ -319,7 +334,7 @@ PagedPlan plan_paged(const Shape &s, int n_rows) {
   p.stage_rows = p.by_rows ? 32 : kStageRows;
   p.col_tiles = (int)((cols + p.tile_cols - 1) / p.tile_cols);
   const int64_t tiles = units * p.col_tiles;
-  int64_t chunks = (p.by_rows ? 1 : 2) * kComputeUnits / tiles, most = (n_rows + (p.by_rows ? 511 : 255)) / (p.by_rows ? 512 : 256);
+  int64_t chunks = (p.by_rows || kTileWaves == 8 ? 1 : 2) * kComputeUnits / tiles, most = (n_rows + (p.by_rows ? 511 : 255)) / (p.by_rows ? 512 : 256);
   if (chunks > most) chunks = most;
   if (chunks > 64) chunks = 64;
   if (chunks < 1) chunks = 1;

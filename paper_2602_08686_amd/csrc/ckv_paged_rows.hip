@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
   f32x16_p acc[I::DTILES];
   auto sweep = [&](auto careful, int mode) {
     constexpr bool CAREFUL = decltype(careful)::value;
-    run = Running{-INFINITY, 0.0f};
+    run = none_yet();
 #pragma unroll
     for (int t = 0; t < I::DTILES; ++t)
 #pragma unroll
@@ -109,7 +109,8 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
           if (block * 32 + row >= c.limit || (missing >> row & 1)) z[r] = -INFINITY;
         }
       }
-      rescale(acc, to_weights<CAREFUL>(z, a.scale2, run, mode));
+      to_weights<CAREFUL>(z, a.scale2, run, mode);
+      rescale(acc, run);
       if (more) wait_vm_at_most<LOADS + 1>();  // V; the next page numbers and K may be on their way
       else wait_vm_at_most<0>();
       second_product<DT, DH, CAREFUL>(v_rows, lane, as_operand<DT>(z), acc, mode);
