@@ -29,8 +29,6 @@ typedef __attribute__((ext_vector_type(4))) float f32x4_p;
 typedef __attribute__((ext_vector_type(4))) short s16x4_p;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_p;
 
-constexpr int kXcdsP = 8;  // accelerator dies of the part; workgroup i of a launch runs on die i % 8
-
 // Four 16-bit words a lane, transposed among 16 lanes: lane i gets word i % 4 of what lanes i / 4, 4 + i / 4, 8 + i / 4, 12 + i / 4 read.
 __device__ __forceinline__ u32x2_p read_transposed(const char *lds) {
   typedef __attribute__((address_space(3))) s16x4_p lds_words;
@@ -82,13 +80,6 @@ __device__ __forceinline__ Column column(const PagedArgs &a, int unit, int tile,
   c.h = g * a.G + col - c.token * a.G;
   c.limit = min(max(max(a.lists.length[unit], 0) - new_rows(a.lists, unit, a.n) + c.token + 1, 0), a.n_rows);
   return c;
-}
-
-// Workgroup `id` of a launch: XCD id % 8 gets a contiguous part of the work, so that the workgroups that read the same
-// rows at the same time share an L2.
-__device__ __forceinline__ int work_item(int id, int total) {
-  const int xcd = id % kXcdsP, at = id / kXcdsP, each = total / kXcdsP, more = total % kXcdsP;
-  return xcd * each + min(xcd, more) + at;
 }
 
 // Over the two lanes (l, l ^ 32) that share a column.

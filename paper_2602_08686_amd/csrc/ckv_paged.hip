@@ -16,10 +16,6 @@
 
 namespace ckv {
 
-#ifndef TW
-#define TW 4
-#endif
-constexpr int kTileWaves = TW;
 constexpr int kStageRows = 64;  // two blocks of 32 rows
 
 // A whole step in bf16, its instructions in the order that they are issued in: slot by slot a matrix product (the two kinds in turn), the operands
@@ -30,10 +26,7 @@ __device__ __forceinline__ void whole_step(const char *k_image, const char *v_im
                                            const f32x16_p &z, f32x16_p &next, Weights<DT> &weights, f32x16_p (&acc)[DH / 32], float scale2, Running &run) {
   constexpr int STEPS = DH / 16, DTILES = DH / 32, SLOTS = 2 * STEPS, MAX_SLOTS = SLOTS / 4, EXP_SLOTS = SLOTS - MAX_SLOTS;
   static_assert(DT == CKV_BF16 && 2 * DTILES == STEPS, "as many products of one kind as of the other");
-  #ifndef AH
-#define AH 2
-#endif
-  constexpr int AHEAD = AH;
+    constexpr int AHEAD = 2;
   const int k_at = k_lane<CKV_BF16, DH>(lane), v_at = v_lane<DH>(lane);
   u32x4_d kf[STEPS], vf[STEPS];
 #pragma unroll
@@ -77,7 +70,7 @@ __device__ __forceinline__ void whole_step(const char *k_image, const char *v_im
 }
 
 template <int DT, int DH, int WAVES>
-__global__ void __launch_bounds__(WAVES *kWave, DH * (DT == CKV_BF16 ? 2 : 4) > 256 ? 1 : 2) paged_tile_kernel(PagedArgs a) {
+__global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && DH == 128 ? 1 : 2) paged_tile_kernel(PagedArgs a) {
   typedef Image<DT, DH> I;
   constexpr int BYTES = kStageRows * I::ROW;
   constexpr int LOADS = BYTES / 1024 / WAVES;       // of K per wave and stage, and of V
@@ -91,10 +84,10 @@ __global__ void __launch_bounds__(WAVES *kWave, DH * (DT == CKV_BF16 ? 2 : 4) > 
   __shared__ Offsets s_at[4][kStageRows];
   __shared__ int s_missing, s_undefined;
 
-  int at = work_item(blockIdx.x, a.workgroups);
-  const int chunk = at % a.n_chunks;
-  at /= a.n_chunks;
-  const int tile = a.col_tiles - 1 - at % a.col_tiles, unit = at / a.col_tiles;  // the longest first
+  // The longest tiles first, of all lists; the lists side by side, so that with a multiple of eight of them a list's workgroups share an L2.
+  const int units = a.workgroups / a.col_tiles / a.n_chunks;
+  const int unit = blockIdx.x % units, chunk = blockIdx.x / units % a.n_chunks;
+  const int tile = a.col_tiles - 1 - blockIdx.x / units / a.n_chunks;
   const int b = unit / a.Hkv, g = unit % a.Hkv;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   const TileRange range = tile_range(a, unit, tile);
@@ -107,6 +100,9 @@ __global__ void __launch_bounds__(WAVES *kWave, DH * (DT == CKV_BF16 ? 2 : 4) > 
   const bool valid = local < range.cols;
   const Column c = column(a, unit, tile, valid ? local : 0);
   const int sees_least = __builtin_amdgcn_readfirstlane(c.limit);  // the wave's first column sees the fewest rows
+  // The wave is through behind the rows that its own columns see.
+  const int sees_most = wave * 32 < range.cols ? column(a, unit, tile, min(range.cols, wave * 32 + 32) - 1).limit : 0;
+  const int own_last = max(min(last, (sees_most + kStageRows - 1) / kStageRows), first + 1);
   u32x4_d qf[I::STEPS];
   load_query<DT, DH>(a, b, c, valid, half, qf);
 
@@ -229,19 +225,20 @@ __global__ void __launch_bounds__(WAVES *kWave, DH * (DT == CKV_BF16 ? 2 : 4) > 
     };
     int stage = first + 1;
 #pragma unroll 1
-    for (; stage + 1 < last; stage += 2) {
+    for (; stage + 1 < own_last; stage += 2) {
       stage_of(std::integral_constant<int, 1>{}, stage);
       stage_of(std::integral_constant<int, 0>{}, stage + 1);
     }
-    if (stage < last) stage_of(std::integral_constant<int, 1>{}, stage);
-    advance(last);
-    const char *v = s_v[(last - 1 - first) & 1];
+    if (stage < own_last) stage_of(std::integral_constant<int, 1>{}, stage);
+    advance(own_last);
+    const char *v = s_v[(own_last - 1 - first) & 1];
     rescale(acc, run);
     second_product<DT, DH, false>(v, lane, weights, acc, kFinite);
-    hide(z, last * kStageRows - 32);
+    hide(z, own_last * kStageRows - 32);
     softmax();
     rescale(acc, run);
     second_product<DT, DH, false>(v + HALF, lane, weights, acc, kFinite);
+    for (stage = own_last + 1; stage <= last; ++stage) advance(stage);  // the other waves' rows, and all barriers
   }
   if (valid && not_finite(acc)) s_undefined = 1;
   __syncthreads();
@@ -326,15 +323,23 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a)
 // ---------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------
+#ifndef RA
+#define RA 512
+#endif
+#ifndef RB
+#define RB 256
+#endif
+#define RR (p.by_rows ? RA : RB)
 PagedPlan plan_paged(const Shape &s, int n_rows) {
   PagedPlan p;
   const int64_t units = (int64_t)s.Bz * s.Hkv, cols = (int64_t)s.G * s.T;
   p.by_rows = cols <= kRowsCols;
-  p.tile_cols = p.by_rows ? kRowsCols : kTileWaves * 32;
+  const int waves = units * ((cols + 255) / 256) >= kComputeUnits ? 8 : 4;
+  p.tile_cols = p.by_rows ? kRowsCols : waves * 32;
   p.stage_rows = p.by_rows ? 32 : kStageRows;
   p.col_tiles = (int)((cols + p.tile_cols - 1) / p.tile_cols);
   const int64_t tiles = units * p.col_tiles;
-  int64_t chunks = (p.by_rows || kTileWaves == 8 ? 1 : 2) * kComputeUnits / tiles, most = (n_rows + (p.by_rows ? 511 : 255)) / (p.by_rows ? 512 : 256);
+  int64_t chunks = (p.by_rows || waves == 8 ? 1 : 2) * kComputeUnits / tiles, most = (n_rows + RR - 1) / RR;
   if (chunks > most) chunks = most;
   if (chunks > 64) chunks = 64;
   if (chunks < 1) chunks = 1;
@@ -344,10 +349,16 @@ PagedPlan plan_paged(const Shape &s, int n_rows) {
   return p;
 }
 
+template <int DT, int DH, int WAVES>
+static void launch_tiles(const PagedArgs &a, hipStream_t stream) {
+  hipLaunchKernelGGL((paged_tile_kernel<DT, DH, WAVES>), dim3((unsigned)a.workgroups), dim3(WAVES * kWave), 0, stream, a);
+}
+
 template <int DT, int DH>
 static void launch_paged_of(const PagedArgs &a, const PagedPlan &plan, int units, hipStream_t stream) {
   if (plan.by_rows) launch_paged_rows(a, DT == CKV_BF16, DH, stream);
-  else hipLaunchKernelGGL((paged_tile_kernel<DT, DH, kTileWaves>), dim3((unsigned)plan.workgroups), dim3(kTileWaves * kWave), 0, stream, a);
+  else if (plan.tile_cols == 256) launch_tiles<DT, DH, 8>(a, stream);
+  else launch_tiles<DT, DH, 4>(a, stream);
   if (plan.n_chunks > 1) {
     constexpr int COLS = kMergeThreads / (DH / 4);
     const unsigned blocks = (unsigned)(a.G * a.n + COLS - 1) / COLS;
@@ -376,6 +387,7 @@ hipError_t launch_paged_attention(const ckv_params *p, const Shape &s, const Pag
                                   const void *k_pages, const void *v_pages, const int32_t *table, const int32_t *length,
                                   const int32_t *count, int n_rows, void *out, const int64_t *out_stride, float *lse, char *ws,
                                   hipStream_t stream) {
+  const int units = s.Bz * s.Hkv;
   PagedArgs a;
   a.q = static_cast<const char *>(q);
   a.k = static_cast<const char *>(k_pages);
@@ -399,7 +411,6 @@ hipError_t launch_paged_attention(const ckv_params *p, const Shape &s, const Pag
   a.n_chunks = plan.n_chunks;
   a.workgroups = (int)plan.workgroups;
   a.scale2 = s.scale * kLog2e;
-  const int units = s.Bz * s.Hkv;
   if (p->dtype == CKV_BF16) {
     if (s.d == 128) launch_paged_of<CKV_BF16, 128>(a, plan, units, stream);
     else launch_paged_of<CKV_BF16, 64>(a, plan, units, stream);

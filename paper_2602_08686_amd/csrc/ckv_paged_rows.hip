@@ -25,10 +25,9 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
   __shared__ float2 s_stats[WAVES][32];
   static_assert(32 * DH * 4 <= 2 * BLOCK, "a wave's sums take its rows' place");
 
-  int at = work_item(blockIdx.x, a.workgroups);
-  const int chunk = at % a.n_chunks;
-  at /= a.n_chunks;
-  const int tile = at % a.col_tiles, unit = at / a.col_tiles;
+  // a list's column tiles, which read the same rows, one behind the other
+  const int units = a.workgroups / a.col_tiles / a.n_chunks;
+  const int unit = blockIdx.x % units, tile = blockIdx.x / units % a.col_tiles, chunk = blockIdx.x / units / a.col_tiles;
   const int b = unit / a.Hkv, g = unit % a.Hkv;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 31, half = lane >> 5;
   const TileRange range = tile_range(a, unit, tile);
