@@ -695,7 +695,7 @@ extern "C" ckv_status ckv_norm_rotate(const ckv_params *params, const ckv_rotati
   if (misaligned({q, k, q_weight, k_weight, q_out, k_out})) return CKV_EINVAL;
   st = rotation_refused(params, rotation, positions, inv_freq);
   if (st != CKV_OK) return st;
-  if ((int64_t)params->batch * params->seq_len > INT32_MAX / 16) return CKV_EUNSUPPORTED;  // workgroups of a launch
+  if ((int64_t)params->batch * params->seq_len > INT32_MAX / 32) return CKV_EUNSUPPORTED;  // workgroups of a launch
   Shape s;
   derive(params, &s);
   if (launch_rows(params, s, rotation, nullptr, q, k, nullptr, positions, inv_freq, q_weight, k_weight, nullptr, nullptr, count, q_out,
@@ -715,7 +715,7 @@ extern "C" ckv_status ckv_paged_append(const ckv_params *params, const ckv_rotat
   st = rotation_refused(params, rotation, positions, inv_freq);
   if (st == CKV_OK) st = pages_refused(params, pages);
   if (st != CKV_OK) return st;
-  if ((int64_t)params->batch * params->seq_len > INT32_MAX / 16) return CKV_EUNSUPPORTED;
+  if ((int64_t)params->batch * params->seq_len > INT32_MAX / 32) return CKV_EUNSUPPORTED;
   Shape s;
   derive(params, &s);
   if (launch_rows(params, s, rotation, pages, q, k, v, positions, inv_freq, q_weight, k_weight, table, length, count, q_out, k_pages,

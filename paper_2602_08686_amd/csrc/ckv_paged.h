@@ -326,6 +326,7 @@ __device__ __forceinline__ void store_lse(const PagedArgs &a, int b, const Colum
 }
 
 constexpr int kRowsCols = 32;  // columns of a tile of paged_rows_kernel
+constexpr int kMostRowsCols = 64;  // up to here it takes a call's columns, in two tiles that read the same rows at the same time
 void launch_paged_rows(const PagedArgs &a, bool bf16, int d, hipStream_t stream);
 
 }  // namespace ckv

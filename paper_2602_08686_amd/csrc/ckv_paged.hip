@@ -292,56 +292,81 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
   }
 }
 
-// Chunks of a column, in their order. A thread takes four components of one column.
-constexpr int kMergeThreads = 256;
+// Chunks of a column, in their order. A column's lanes take four components each, and for the weights a chunk each; loads of eight chunks are in flight
+// together (one after the other, sixteen chunks took 12 us, now 5).
+constexpr int kMergeThreads = 256, kMostChunks = 64;
 template <int DT, int DH>
 __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a) {
-  constexpr int PIECES = DH / 4, COLS = kMergeThreads / PIECES;
+  constexpr int PIECES = DH / 4, COLS = kMergeThreads / PIECES, SHARE = kMostChunks / PIECES;
   const int blocks = (a.G * a.n + COLS - 1) / COLS;
-  const int unit = blockIdx.x / blocks, col = blockIdx.x % blocks * COLS + threadIdx.x / PIECES, d = threadIdx.x % PIECES * 4;
-  if (col >= a.G * new_rows(a.lists, unit, a.n)) return;
+  const int unit = blockIdx.x / blocks, col = blockIdx.x % blocks * COLS + threadIdx.x / PIECES, piece = threadIdx.x % PIECES;
+  const bool valid = col < a.G * new_rows(a.lists, unit, a.n);
   const int tile = col / a.tile_cols, local = col % a.tile_cols, b = unit / a.Hkv;
   const TileRange range = tile_range(a, unit, tile);
-  const int chunks = (range.stages + range.per_chunk - 1) / range.per_chunk;
+  const int chunks = valid ? (range.stages + range.per_chunk - 1) / range.per_chunk : 0;
   const size_t first = ((size_t)unit * a.col_tiles + tile) * a.n_chunks * a.tile_cols + local;
-  float top = -INFINITY, sum = 0.0f;
-  for (int i = 0; i < chunks; ++i) top = fmaxf(top, a.stats[first + (size_t)i * a.tile_cols].x);
-  const float ref = top == -INFINITY ? 0.0f : top;
-  f32x4_p num = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = 0; i < chunks; ++i) {
-    const size_t row = first + (size_t)i * a.tile_cols;
-    const float2 st = a.stats[row];
-    const float f = __builtin_amdgcn_exp2f(st.x - ref);
-    sum = fmaf(st.y, f, sum);
-    num = add_part(num, *reinterpret_cast<const f32x4_p *>(a.part + row * DH + d), f);
+  float2 st[SHARE];
+  float top = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < SHARE; ++k) {
+    const int i = k * PIECES + piece;
+    st[k] = make_float2(-INFINITY, 0.0f);
+    if (i < chunks) st[k] = a.stats[first + (size_t)i * a.tile_cols];
+    top = fmaxf(top, st[k].x);
   }
+#pragma unroll
+  for (int o = 1; o < PIECES; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f, weight[SHARE];
+#pragma unroll
+  for (int k = 0; k < SHARE; ++k) {
+    weight[k] = __builtin_amdgcn_exp2f(st[k].x - ref);
+    sum = fmaf(st[k].y, weight[k], sum);
+  }
+#pragma unroll
+  for (int o = 1; o < PIECES; o <<= 1) sum += __shfl_xor(sum, o);
+  f32x4_p num = {0.0f, 0.0f, 0.0f, 0.0f};
+  constexpr int BATCH = 8;
+#pragma unroll
+  for (int k = 0; k < SHARE; ++k) {
+    for (int c0 = 0; c0 < PIECES && k * PIECES + c0 < a.n_chunks; c0 += BATCH) {  // the same for all lanes
+      f32x4_p x[BATCH];
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        const int i = k * PIECES + c0 + j;
+        x[j] = f32x4_p{0.0f, 0.0f, 0.0f, 0.0f};
+        if (i < chunks) x[j] = *reinterpret_cast<const f32x4_p *>(a.part + (first + (size_t)i * a.tile_cols) * DH + 4 * piece);
+      }
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) num = add_part(num, x[j], __shfl(weight[k], (threadIdx.x & 63) / PIECES * PIECES + c0 + j));
+    }
+  }
+  if (!valid) return;
   const Column c = column(a, unit, tile, local);
-  store_out<DT>(out_row(a, b, c), d, num * inverse_sum(sum));
-  if (d == 0) store_lse(a, b, c, top, sum);
+  store_out<DT>(out_row(a, b, c), 4 * piece, num * inverse_sum(sum));
+  if (piece == 0) store_lse(a, b, c, top, sum);
 }
 
 // ---------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------
-#ifndef RA
-#define RA 512
-#endif
-#ifndef RB
-#define RB 256
-#endif
-#define RR (p.by_rows ? RA : RB)
+// Workgroups along the rows: as many as fill the chip (one of eight waves a CU, or two of four), if each of them has enough rows to be worth
+// the way through memory that its sums then take, and none beside the first for so few rows that the merge would cost more than it saves.
 PagedPlan plan_paged(const Shape &s, int n_rows) {
   PagedPlan p;
+  const bool bf16 = s.esize == 2;
   const int64_t units = (int64_t)s.Bz * s.Hkv, cols = (int64_t)s.G * s.T;
-  p.by_rows = cols <= kRowsCols;
+  p.by_rows = cols <= kMostRowsCols;
   const int waves = units * ((cols + 255) / 256) >= kComputeUnits ? 8 : 4;
   p.tile_cols = p.by_rows ? kRowsCols : waves * 32;
   p.stage_rows = p.by_rows ? 32 : kStageRows;
   p.col_tiles = (int)((cols + p.tile_cols - 1) / p.tile_cols);
   const int64_t tiles = units * p.col_tiles;
-  int64_t chunks = (p.by_rows || waves == 8 ? 1 : 2) * kComputeUnits / tiles, most = (n_rows + RR - 1) / RR;
+  int64_t chunks = (p.by_rows || waves == 8 ? 1 : 2) * kComputeUnits / tiles;
+  const int least = p.by_rows ? (bf16 ? 256 : 128) : (bf16 ? 512 : 128);
+  const int64_t most = p.by_rows && n_rows <= (bf16 ? 1024 : 256) ? 1 : (n_rows + least - 1) / least;
   if (chunks > most) chunks = most;
-  if (chunks > 64) chunks = 64;
+  if (chunks > kMostChunks) chunks = kMostChunks;
   if (chunks < 1) chunks = 1;
   p.n_chunks = (int)chunks;
   p.workgroups = tiles * chunks;

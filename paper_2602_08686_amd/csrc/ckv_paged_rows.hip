@@ -16,7 +16,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
   constexpr int LOADS = 32 / I::ROWS_PER_LOAD;  // of K, and of V, per block
   constexpr int BLOCK = 32 * I::ROW;
   constexpr int PIECES = DH / 4;                // of 16 bytes of a column's fp32 sums
-  __shared__ __align__(1024) char s_rows[WAVES][2][BLOCK];
+  __shared__ __align__(1024) char s_rows[WAVES][2 * BLOCK];  // K's rows, V's rows
   __shared__ __align__(256) int32_t s_ids[WAVES][2][kWave];
   struct Offsets {
     int64_t k, v;
@@ -30,26 +30,33 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
   const int unit = blockIdx.x % units, tile = blockIdx.x / units % a.col_tiles, chunk = blockIdx.x / units / a.col_tiles;
   const int b = unit / a.Hkv, g = unit % a.Hkv;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 31, half = lane >> 5;
-  const TileRange range = tile_range(a, unit, tile);
-  if (range.cols <= 0) return;
-  const int first = chunk * range.per_chunk, last = min(first + range.per_chunk, range.stages);  // blocks of 32 rows
   const bool single = a.n_chunks == 1;
-  if (first >= last && !single) return;  // the merge reads the chunks that have blocks
+  const int32_t *list = a.lists.table + b * a.lists.table_b + g * a.lists.table_h;
+  const char *kb = a.k + g * a.lists.ks[1], *vb = a.v + g * a.lists.vs[1];
+  // A single workgroup knows its first rows before it knows the length: their page numbers come beside it.
+  // Page numbers of a block, from the list alone; rows behind the end are the last one again, and a page that is not in the pool is page 0
+  // (they weigh nothing).
+  auto fetch_ids = [&](int block, int slot) { dma_4(list + (min(block * 32 + m, a.n_rows - 1) >> a.lists.shift), s_ids[wave][slot]); };
+  if (single) {
+    fetch_ids(wave, 0);
+    fetch_ids(wave + WAVES, 1);
+  }
+  const TileRange range = tile_range(a, unit, tile);
+  const int first = chunk * range.per_chunk, last = min(first + range.per_chunk, range.stages);  // blocks of 32 rows
+  if (range.cols <= 0 || (first >= last && !single)) {  // the merge reads the chunks that have blocks
+    wait_vm_at_most<0>();
+    return;
+  }
 
   const bool valid = m < range.cols;
   const Column c = column(a, unit, tile, valid ? m : 0);
   const int sees_least = __builtin_amdgcn_readfirstlane(c.limit);
   u32x4_d qf[I::STEPS];
   load_query<DT, DH>(a, b, c, valid, half, qf);
-
-  const int32_t *list = a.lists.table + b * a.lists.table_b + g * a.lists.table_h;
-  const char *kb = a.k + g * a.lists.ks[1], *vb = a.v + g * a.lists.vs[1];
-  char *k_rows = s_rows[wave][0], *v_rows = s_rows[wave][1];
-  // Rows behind the end are the last one again; a page that is not in the pool is page 0 (they weigh nothing).
-  auto row_of = [&](int block) { return min(block * 32 + m, range.end - 1); };
-  auto fetch_ids = [&](int block, int slot) { dma_4(list + (row_of(block) >> a.lists.shift), s_ids[wave][slot]); };
+  char *k_rows = s_rows[wave], *v_rows = s_rows[wave] + BLOCK;
   auto find_rows = [&](int block, int slot) {  // returns which of the 32 are on no page
-    const int id = s_ids[wave][slot][m], row = row_of(block) & ((1 << a.lists.shift) - 1);
+    const int at = min(m, range.end - 1 - block * 32);
+    const int id = s_ids[wave][slot][at], row = (block * 32 + at) & ((1 << a.lists.shift) - 1);
     const bool ok = (unsigned)id < (unsigned)a.lists.n_pages;
     const int64_t page = ok ? id : 0;
     if (half == 0) s_at[wave][m] = Offsets{page * a.lists.ks[0] + row * a.lists.ks[2], page * a.lists.vs[0] + row * a.lists.vs[2]};
@@ -83,9 +90,11 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
       for (int r = 0; r < 16; ++r) acc[t][r] = 0.0f;
     int block = first + wave, slot = 0;
     if (block >= last) return;
-    fetch_ids(block, 0);
-    fetch_ids(block + WAVES, 1);
-    wait_vm_at_most<1>();
+    if (!single || CAREFUL) {
+      fetch_ids(block, 0);
+      fetch_ids(block + WAVES, 1);
+    }
+    wait_vm_at_most<0>();
     uint32_t missing = find_rows(block, 0);
     fetch_k();
     fetch_v();
@@ -130,7 +139,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
 
   // the waves' sums in their rows' places, the pieces of a column permuted by it
   if (valid) {
-    char *to = s_rows[wave][0] + m * DH * 4;
+    char *to = s_rows[wave] + m * DH * 4;
 #pragma unroll
     for (int t = 0; t < I::DTILES; ++t)
 #pragma unroll
@@ -153,7 +162,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
       const float2 st = s_stats[w][local];
       const float f = __builtin_amdgcn_exp2f(st.x - ref);
       sum = fmaf(st.y, f, sum);
-      num = add_part(num, *reinterpret_cast<const f32x4_p *>(s_rows[w][0] + local * DH * 4 + ((piece ^ local) % PIECES) * 16), f);
+      num = add_part(num, *reinterpret_cast<const f32x4_p *>(s_rows[w] + local * DH * 4 + ((piece ^ local) % PIECES) * 16), f);
     }
     if (single) {
       const Column o = column(a, unit, tile, local);

@@ -1,10 +1,13 @@
 // New rows on their way into a cache: RMS norm of every head, position rotation, and the place in the pages.
 //
-// Bound by memory: every row read once and written once, 2 * d * e bytes of it. A workgroup takes a few tokens of a sequence: it makes
-// the cosines and sines of their angles once, in LDS (a token's angles are those of all its heads), and its heads' rows go through
-// registers, eight components a lane. A lane of the rotated front holds four components and their four partners, so that no lane needs
-// another's: halves (c, c + rot/2) lie in two pieces of four, neighbours in eight consecutive ones. Sums of squares cross the row's
-// lanes as operands of the additions. Rows without norm and rotation (values; keys that the retention step kept) are copied as bits.
+// Bound by memory: every row read once and written once, 2 * d * e bytes of it; on the way there, the address arithmetic costs more than the
+// rotation. So a workgroup takes a few tokens of a sequence with some of their KV heads, and first makes, in LDS, what all lanes
+// of its rows need: the cosines and sines of each token's angles (the same for all its heads) and, a thread for each (token, KV
+// head), where its rows come from and go to, page numbers looked up. Then 8 or 16 lanes take a (token, KV head): the key, the value and the
+// group's queries go through registers, eight components a lane, all their loads in flight together. A lane of the rotated
+// front holds four components and their four partners, so that no lane needs another's: halves (c, c + rot/2) lie in two pieces of
+// four, neighbours in eight consecutive ones. Sums of squares cross the row's lanes as operands of the additions. Rows without
+// norm and rotation (values; keys that the retention step kept) are copied as bits.
 //
 // Angles: position * inv_freq / (2 pi) in fp64, off by less than 2^-51 of itself (2^-31 of a turn a million turns away), and without
 // its whole turns to fp32.
@@ -23,15 +26,15 @@ struct RowsArgs {
   int Hq, Hkv, G, n;
   int rot, norm;
   float eps;
-  int q_rows, k_rows, rows;        // rows of a token: queries, keys, and all (values behind the keys)
-  int tokens, token_blocks;        // tokens of a workgroup, workgroups along a sequence
-  int split_rows;                  // rows of a token that one workgroup takes (grid.y of them)
+  int tokens, token_blocks;        // tokens of a workgroup (a power of two), workgroups along a sequence
+  int heads;                       // KV heads of a workgroup (grid.y of them)
 };
 
 constexpr int kRowThreads = 256;
 constexpr int kMostTokens = 8;     // tokens of a workgroup
+constexpr int kMostHeads = kRowThreads / kMostTokens;  // KV heads: a thread for every (token, head)
 
-// Eight components in two pieces of four, as fp32.
+// Four components as fp32, and back: to the nearest, ties to even, the one rounding of a row's way.
 template <int DT>
 __device__ __forceinline__ void load_four(const char *p, float *x) {
   if (DT == CKV_BF16) {
@@ -50,7 +53,7 @@ __device__ __forceinline__ void load_four(const char *p, float *x) {
 }
 template <int DT>
 __device__ __forceinline__ void store_four(char *p, const float *x) {
-  if (DT == CKV_BF16) {  // the one rounding: to the nearest, ties to even
+  if (DT == CKV_BF16) {
     *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
   } else {
     *reinterpret_cast<uint4 *>(p) =
@@ -59,140 +62,163 @@ __device__ __forceinline__ void store_four(char *p, const float *x) {
 }
 
 enum RowForm { kCopied, kHalves, kNeighbours };  // what happens to keys and queries: nothing, or norm and rotation in these pairs
-// U: rows whose loads a lane has in flight.
+
+// Eight components of a row in a lane, at `at0` and `at1` bytes (four each), or as they are.
+template <int DT, int DH, int FORM>
+struct LaneRow {
+  static constexpr int ESIZE = DT == CKV_BF16 ? 2 : 4, LPR = DH / 8;
+  static constexpr bool NEIGHBOURS = FORM == kNeighbours;
+  float x[8];
+  __device__ __forceinline__ void load(const char *row, int at0, int at1) {
+    load_four<DT>(row + at0, &x[0]);
+    load_four<DT>(row + at1, &x[4]);
+  }
+  // all lanes of the row take part
+  __device__ __forceinline__ void change(bool norm, float eps, const float (&w)[8], bool turned, const float2 (&turn)[4]) {
+    if (norm) {
+      float sq = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sq = fmaf(x[e], x[e], sq);
+      sq = row_sum<LPR>(sq);
+      const float f = __builtin_amdgcn_rsqf(fmaf(sq, 1.0f / DH, eps));  // one unit of the last place
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = x[e] * f * w[e];
+    }
+    if (turned) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        // the pair's two components: (e, 4 + e) of the pieces, or neighbours
+        float &p = NEIGHBOURS ? x[2 * e] : x[e], &p2 = NEIGHBOURS ? x[2 * e + 1] : x[4 + e];
+        const float y = p, y2 = p2;
+        p = y * turn[e].x - y2 * turn[e].y;
+        p2 = y2 * turn[e].x + y * turn[e].y;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char *row, int at0, int at1) const {
+    store_four<DT>(row + at0, &x[0]);
+    store_four<DT>(row + at1, &x[4]);
+  }
+};
+template <int DT, int DH>
+struct LaneRow<DT, DH, kCopied> {
+  static constexpr int WORDS = DT == CKV_BF16 ? 1 : 2;
+  u32x4_d x[WORDS];
+  __device__ __forceinline__ void load(const char *row, int at0, int) {
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) x[w] = *reinterpret_cast<const u32x4_d *>(row + at0 + 16 * w);
+  }
+  __device__ __forceinline__ void change(bool, float, const float (&)[8], bool, const float2 (&)[4]) {}
+  __device__ __forceinline__ void store(char *row, int at0, int) const {
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) *reinterpret_cast<u32x4_d *>(row + at0 + 16 * w) = x[w];
+  }
+};
+
 // PAGED: keys and values go into pages, else keys are dense and there are no values.
-template <int DT, int DH, int FORM, bool PAGED, int U>
+template <int DT, int DH, int FORM, bool PAGED>
 __global__ void __launch_bounds__(kRowThreads) rows_kernel(RowsArgs a) {
-  constexpr bool TRANSFORM = FORM != kCopied, NEIGHBOURS = FORM == kNeighbours;
+  constexpr bool TRANSFORM = FORM != kCopied;
   constexpr int ESIZE = DT == CKV_BF16 ? 2 : 4, ROW = DH * ESIZE;
   constexpr int LPR = DH / 8;                 // lanes of a row
-  constexpr int ABREAST = kRowThreads / LPR;  // rows at a time
-  constexpr int PIECE = 4 * ESIZE;
+  constexpr int ABREAST = kRowThreads / LPR;  // (token, KV head)s at a time
+  constexpr int Q = 4;                        // queries whose loads are in flight together
   __shared__ float2 s_turn[kMostTokens][TRANSFORM ? DH / 2 : 1];  // cosine and sine
+  struct Way {                                // BYTES from the tensors' starts
+    int64_t q, k, v, q_out, k_out, v_out;
+    int32_t here, placed;                     // the row is one of the call's; k_out and v_out are in the pools
+  };
+  __shared__ Way s_way[kRowThreads];
   const int b = blockIdx.x / a.token_blocks, first = (blockIdx.x % a.token_blocks) * a.tokens;
-  const int tokens = min(a.tokens, a.n - first);
-  const int r0 = blockIdx.y * a.split_rows, split = min(a.split_rows, a.rows - r0);
+  const int g0 = blockIdx.y * a.heads, heads = min(a.heads, a.Hkv - g0), ways = a.tokens * heads;
   const int sub = threadIdx.x % LPR, slot = threadIdx.x / LPR;
 
+  if ((int)threadIdx.x < ways) {
+    const int i = first + threadIdx.x % a.tokens, g = g0 + threadIdx.x / a.tokens, unit = b * a.Hkv + g, h = g * a.G;
+    const int count = new_rows(a.lists, unit, a.n);
+    Way w;
+    w.here = i < min(count, a.n);
+    w.placed = w.here;
+    w.q = b * a.qs[0] + h * a.qs[1] + i * a.qs[2];
+    w.k = b * a.ks[0] + g * a.ks[1] + i * a.ks[2];
+    w.v = b * a.vs[0] + g * a.vs[1] + i * a.vs[2];
+    w.q_out = (((int64_t)b * a.Hq + h) * a.n + i) * ROW;
+    w.k_out = ((int64_t)unit * a.n + i) * ROW;
+    w.v_out = 0;
+    if (PAGED && w.here) {
+      const int at = max(a.lists.length[unit], 0) - count + i;
+      w.placed = at >= 0 && at < a.lists.capacity;
+      if (w.placed) {
+        const int page = a.lists.table[b * a.lists.table_b + g * a.lists.table_h + (at >> a.lists.shift)], row = at & ((1 << a.lists.shift) - 1);
+        w.placed = (unsigned)page < (unsigned)a.lists.n_pages;
+        w.k_out = in_pool(a.lists.ks, page, g, row);
+        w.v_out = in_pool(a.lists.vs, page, g, row);
+      }
+    }
+    s_way[threadIdx.x] = w;
+  }
   if (TRANSFORM && a.rot > 0) {
-    const int half = a.rot / 2;
+    const int half = a.rot / 2, tokens = min(a.tokens, a.n - first);
     for (int i = threadIdx.x; i < tokens * half; i += kRowThreads) {
-      const int t = i / half, c = i % half;
+      const int t = i / half, c = i - t * half;
       const double turns = (double)a.positions[(size_t)b * a.n + first + t] * (double)a.inv_freq[c] * 0.15915494309189535;
       float2 cs;
       sincospif(2.0f * (float)(turns - rint(turns)), &cs.y, &cs.x);
       s_turn[t][c] = cs;
     }
-    __syncthreads();
   }
+  __syncthreads();
 
   // pieces of the lane: bytes from the row's start
   const bool turned = TRANSFORM && sub < a.rot / 8;
-  const bool apart = turned && !NEIGHBOURS;
+  const bool apart = turned && FORM == kHalves;
   const int at0 = apart ? 4 * sub * ESIZE : 8 * sub * ESIZE;
-  const int at1 = apart ? (a.rot / 2 + 4 * sub) * ESIZE : at0 + PIECE;
+  const int at1 = apart ? (a.rot / 2 + 4 * sub) * ESIZE : at0 + 4 * ESIZE;
   float qw[8], kw[8];
-  if (TRANSFORM) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) qw[e] = kw[e] = 1.0f;
-    if (a.norm && a.q_weight) {
-      load_four<DT>(static_cast<const char *>(a.q_weight) + at0, &qw[0]);
-      load_four<DT>(static_cast<const char *>(a.q_weight) + at1, &qw[4]);
-    }
-    if (a.norm && a.k_weight) {
-      load_four<DT>(static_cast<const char *>(a.k_weight) + at0, &kw[0]);
-      load_four<DT>(static_cast<const char *>(a.k_weight) + at1, &kw[4]);
-    }
+  for (int e = 0; e < 8; ++e) qw[e] = kw[e] = 1.0f;
+  if (TRANSFORM && a.norm && a.q_weight) {
+    load_four<DT>(static_cast<const char *>(a.q_weight) + at0, &qw[0]);
+    load_four<DT>(static_cast<const char *>(a.q_weight) + at1, &qw[4]);
+  }
+  if (TRANSFORM && a.norm && a.k_weight) {
+    load_four<DT>(static_cast<const char *>(a.k_weight) + at0, &kw[0]);
+    load_four<DT>(static_cast<const char *>(a.k_weight) + at1, &kw[4]);
   }
 
-  // rows of the workgroup in the order (token, row of the token), ABREAST of them at a time
-  int t = slot / split, r = slot % split;
-  while (t < tokens) {
-    float x[U][8];
-    u32x4_d raw[U][ESIZE / 2];
-    char *to[U];       // where the row goes, or null
-    bool here[U], keys[U], copied[U];
-    int token[U];
+  for (int i = slot; i < ways; i += ABREAST) {
+    const Way &w = s_way[i];
+    if (!w.here) continue;  // a row's lanes all go on or none does
+    LaneRow<DT, DH, FORM> key, query[Q];
+    LaneRow<DT, DH, kCopied> value;
+    const char *from = a.q + w.q;
+    char *to = a.q_out + w.q_out;
+    const int64_t to_step = (int64_t)a.n * ROW;
+    if (a.k) key.load(a.k + w.k, at0, at1);
+    if (PAGED) value.load(a.v + w.v, 8 * sub * ESIZE, 0);
+    const int queries = a.q ? a.G : 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      to[u] = nullptr;
-      here[u] = keys[u] = false;
-      copied[u] = !TRANSFORM;
-      token[u] = t;
-      if (t < tokens) {
-        const int row = r0 + r, i = first + t;
-        const bool query = row < a.q_rows;
-        keys[u] = !query && row < a.q_rows + a.k_rows;
-        copied[u] = !TRANSFORM || (!query && !keys[u]);
-        const int h = query ? row : row - a.q_rows - (keys[u] ? 0 : a.k_rows), g = query ? h / a.G : h, unit = b * a.Hkv + g;
-        const int count = new_rows(a.lists, unit, a.n);
-        here[u] = i < count;
-        if (here[u]) {
-          const char *src = query ? a.q + b * a.qs[0] + h * a.qs[1] + i * a.qs[2]
-                          : keys[u] ? a.k + b * a.ks[0] + h * a.ks[1] + i * a.ks[2]
-                                    : a.v + b * a.vs[0] + h * a.vs[1] + i * a.vs[2];
-          if (copied[u]) {
+    for (int h = 0; h < Q; ++h)
+      if (h < queries) query[h].load(from + h * a.qs[1], at0, at1);
+    float2 turn[4];
+    if (turned) {
 #pragma unroll
-            for (int w = 0; w < ESIZE / 2; ++w) raw[u][w] = *reinterpret_cast<const u32x4_d *>(src + sub * 8 * ESIZE + 16 * w);
-          } else {
-            load_four<DT>(src + at0, &x[u][0]);
-            load_four<DT>(src + at1, &x[u][4]);
-          }
-          if (query) {
-            to[u] = a.q_out + (((size_t)b * a.Hq + h) * a.n + i) * ROW;
-          } else if (!PAGED) {
-            to[u] = a.k_out + ((size_t)unit * a.n + i) * ROW;
-          } else {
-            const int at = max(a.lists.length[unit], 0) - count + i;
-            if (at >= 0 && at < a.lists.capacity) {
-              const int page = a.lists.table[b * a.lists.table_b + g * a.lists.table_h + (at >> a.lists.shift)];
-              const int in_page = at & ((1 << a.lists.shift) - 1);
-              if ((unsigned)page < (unsigned)a.lists.n_pages)
-                to[u] = keys[u] ? a.k_out + in_pool(a.lists.ks, page, g, in_page) : a.v_out + in_pool(a.lists.vs, page, g, in_page);
-            }
-          }
-        }
-      }
-      r += ABREAST;
-      while (r >= split) {
-        r -= split;
-        ++t;
-      }
+      for (int e = 0; e < 4; ++e) turn[e] = s_turn[i % a.tokens][4 * sub + e];
     }
+    if (a.k) {
+      key.change(a.norm, a.eps, kw, turned, turn);
+      if (w.placed) key.store(a.k_out + w.k_out, at0, at1);
+    }
+    if (PAGED && w.placed) value.store(a.v_out + w.v_out, 8 * sub * ESIZE, 0);
+    for (int h0 = 0; h0 < queries; h0 += Q) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (TRANSFORM && a.norm) {
-        float sq = 0.0f;
-        if (here[u] && !copied[u]) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sq = fmaf(x[u][e], x[u][e], sq);
-        }
-        sq = row_sum<LPR>(sq);  // a row's lanes are all here or none is
-        if (here[u] && !copied[u]) {
-          const float f = 1.0f / sqrtf(sq * (1.0f / DH) + a.eps);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[u][e] = x[u][e] * f * (keys[u] ? kw[e] : qw[e]);
-        }
-      }
-      if (!to[u]) continue;
-      if (copied[u]) {
-#pragma unroll
-        for (int w = 0; w < ESIZE / 2; ++w) *reinterpret_cast<u32x4_d *>(to[u] + sub * 8 * ESIZE + 16 * w) = raw[u][w];
-        continue;
-      }
-      if (turned) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 cs = s_turn[token[u]][4 * sub + e];
-          // the pair's two components: (e, 4 + e) of the pieces, or neighbours
-          float &p = NEIGHBOURS ? x[u][2 * e] : x[u][e], &p2 = NEIGHBOURS ? x[u][2 * e + 1] : x[u][4 + e];
-          const float y = p, y2 = p2;
-          p = y * cs.x - y2 * cs.y;
-          p2 = y2 * cs.x + y * cs.y;
+      for (int h = 0; h < Q; ++h) {
+        if (h0 + h < queries) {
+          query[h].change(a.norm, a.eps, qw, turned, turn);
+          query[h].store(to + (h0 + h) * to_step, at0, at1);
+          if (h0 + Q + h < queries) query[h].load(from + (h0 + Q + h) * a.qs[1], at0, at1);
         }
       }
-      store_four<DT>(to[u] + at0, &x[u][0]);
-      store_four<DT>(to[u] + at1, &x[u][4]);
     }
   }
 }
@@ -202,8 +228,8 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(RowsArgs a) {
 // ---------------------------------------------------------------------------------------------
 template <int DT, int DH, int FORM>
 static void launch_rows_as(const RowsArgs &a, dim3 grid, bool paged, hipStream_t stream) {
-  if (paged) hipLaunchKernelGGL((rows_kernel<DT, DH, FORM, true, 4>), grid, dim3(kRowThreads), 0, stream, a);
-  else hipLaunchKernelGGL((rows_kernel<DT, DH, FORM, false, 4>), grid, dim3(kRowThreads), 0, stream, a);
+  if (paged) hipLaunchKernelGGL((rows_kernel<DT, DH, FORM, true>), grid, dim3(kRowThreads), 0, stream, a);
+  else hipLaunchKernelGGL((rows_kernel<DT, DH, FORM, false>), grid, dim3(kRowThreads), 0, stream, a);
 }
 template <int DT, int DH>
 static void launch_rows_of(const RowsArgs &a, dim3 grid, RowForm form, bool paged, hipStream_t stream) {
@@ -241,22 +267,16 @@ hipError_t launch_rows(const ckv_params *p, const Shape &s, const ckv_rotation *
   a.rot = rotation ? rotation->rot_dim : 0;
   a.norm = rotation ? rotation->norm : 0;
   a.eps = rotation ? rotation->norm_eps : 0.0f;
-  a.q_rows = q ? s.Hq : 0;
-  a.k_rows = k ? s.Hkv : 0;
-  a.rows = a.q_rows + a.k_rows + (v ? s.Hkv : 0);
-  // Long calls: a few tokens a workgroup, so that the angles are made once for all heads. Short ones: a token's rows over
-  // several workgroups, each of which makes the angles again.
-  const int abreast = kRowThreads / (s.d / 8);
+  // Long calls: a few tokens a workgroup, so that the angles are made once for all heads. Short ones: a token's heads over several workgroups, each
+  // of which makes the angles again.
   const int64_t tokens = (int64_t)s.Bz * s.T;
   a.tokens = 1;
-  while (a.tokens < kMostTokens && tokens / (2 * a.tokens) >= 4 * kComputeUnits) a.tokens *= 2;
+  while (a.tokens < kMostTokens && 2 * a.tokens <= s.T && tokens / (2 * a.tokens) >= 4 * kComputeUnits) a.tokens *= 2;
   a.token_blocks = (s.T + a.tokens - 1) / a.tokens;
   const int64_t blocks = (int64_t)s.Bz * a.token_blocks;
-  int splits = 1;
-  while (blocks * splits < 2 * kComputeUnits && splits * abreast < a.rows) ++splits;
-  a.split_rows = (a.rows + splits - 1) / splits;
-  splits = (a.rows + a.split_rows - 1) / a.split_rows;
-  const dim3 grid((unsigned)blocks, (unsigned)splits);
+  a.heads = s.Hkv < kMostHeads ? s.Hkv : kMostHeads;
+  while (a.heads > 1 && blocks * ((s.Hkv + a.heads - 1) / a.heads) < kComputeUnits) a.heads = (a.heads + 1) / 2;
+  const dim3 grid((unsigned)blocks, (unsigned)((s.Hkv + a.heads - 1) / a.heads));
   const RowForm form = a.rot == 0 && !a.norm ? kCopied : a.rot > 0 && rotation->pairing == CKV_PAIR_NEIGHBOURS ? kNeighbours : kHalves;
   if (p->dtype == CKV_BF16) {
     if (s.d == 128) launch_rows_of<CKV_BF16, 128>(a, grid, form, pages != nullptr, stream);

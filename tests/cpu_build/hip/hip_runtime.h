@@ -104,6 +104,7 @@ inline int __any(int p) { return __ballot(p) != 0; }
 #define __builtin_amdgcn_readlane(x, l) emu::from((int)(x), l)
 #define __builtin_amdgcn_readfirstlane(x) emu::from((int)(x), __builtin_ctzll(emu::live()))
 #define __builtin_amdgcn_exp2f(x) exp2f(x)
+#define __builtin_amdgcn_rsqf(x) (1.0f / sqrtf(x))
 #define __builtin_amdgcn_sched_barrier(x) ((void)0)
 #define __builtin_amdgcn_permlane16_swap(x, y, a, b) emu::swap_halves(x, y, 16)
 #define __builtin_amdgcn_permlane32_swap(x, y, a, b) emu::swap_halves(x, y, 32)
