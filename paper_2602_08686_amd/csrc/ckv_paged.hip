@@ -113,11 +113,11 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
 
   // Where the rows of a stage are: one wave, another for every stage, turns its page numbers into offsets, two stages ahead of the first loads that
   // need them. Rows behind the end are the last one again; a page that is not in the pool is page 0 (they weigh nothing).
-  auto row_of = [&](int stage) { return min(stage * kStageRows + lane, range.end - 1); };
-  auto fetch_ids = [&](int stage) {
+  auto row_of = [&](int stage) CKV_INLINE { return min(stage * kStageRows + lane, range.end - 1); };
+  auto fetch_ids = [&](int stage) CKV_INLINE {
     if (wave == stage % WAVES) dma_4(list + (row_of(stage) >> a.lists.shift), s_ids[stage & 1]);
   };
-  auto find_rows = [&](int stage) {
+  auto find_rows = [&](int stage) CKV_INLINE {
     if (wave != stage % WAVES) return;
     const int id = s_ids[stage & 1][lane], row = row_of(stage) & ((1 << a.lists.shift) - 1);
     const bool ok = (unsigned)id < (unsigned)a.lists.n_pages;
@@ -125,14 +125,14 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
     if (!ok) s_missing = 1;
     s_at[stage & 3][lane] = Offsets{page * a.lists.ks[0] + row * a.lists.ks[2], page * a.lists.vs[0] + row * a.lists.vs[2]};
   };
-  auto fetch_k = [&](int stage) {
+  auto fetch_k = [&](int stage) CKV_INLINE {
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       const int row = (wave * LOADS + j) * I::ROWS_PER_LOAD + lane / I::PIECES;
       dma_16<false>(kb + s_at[stage & 3][row].k + I::k_piece(row, lane % I::PIECES) * 16, s_k[(stage - first) & 1] + (wave * LOADS + j) * 1024);
     }
   };
-  auto fetch_v = [&](int stage) {
+  auto fetch_v = [&](int stage) CKV_INLINE {
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       const int row = (wave * LOADS + j) * I::ROWS_PER_LOAD + lane / I::PIECES;
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
 
   Running run;
   f32x16_p acc[I::DTILES];
-  auto begin = [&]() {
+  auto begin = [&]() CKV_INLINE {
     run = none_yet();
 #pragma unroll
     for (int t = 0; t < I::DTILES; ++t)
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
       for (int r = 0; r < 16; ++r) acc[t][r] = 0.0f;
   };
   // logits of rows that the column does not see
-  auto hide = [&](f32x16_p &z, int z_row) {
+  auto hide = [&](f32x16_p &z, int z_row) CKV_INLINE {
     if (!s_missing && z_row + 32 <= sees_least) return;
     const int sees = c.limit - z_row - 4 * half;  // rows of the block from the half's first one on
     uint32_t there = ~0u;
@@ -183,11 +183,11 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
     // Steps of the pipeline: the first product of a block, the softmax of the one before, the second product of the one before that, none
     // of which waits for another: the matrix cores have work while the vector units are at the softmax. What is a branch comes in
     // front, so that the rest is one block of instructions to be scheduled.
-    auto softmax = [&]() {
+    auto softmax = [&]() CKV_INLINE {
       to_weights<false>(z, a.scale2, run, kFinite);
       weights = as_operand<DT>(z);
     };
-    auto step = [&](const char *k_image, int z_row, const char *v_image) {
+    auto step = [&](const char *k_image, int z_row, const char *v_image) CKV_INLINE {
       rescale(acc, run);
       hide(z, z_row);
       f32x16_p next;
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
       pin(weights, run.sum);  // or the exponentials move behind the next step's branch, away from these products
       z = next;
     };
-    auto advance = [&](int stage) {
+    auto advance = [&](int stage) CKV_INLINE {
       wait_vm_at_most<0>();
       __syncthreads();  // K of this stage and V of the one before are there, and the buffers of the next loads have been read
       if (stage + 2 < last) find_rows(stage + 2);
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
     softmax();
     z = next;
     // buffers known at compile time: operands at fixed offsets from a few addresses
-    auto stage_of = [&](auto parity, int stage) {
+    auto stage_of = [&](auto parity, int stage) CKV_INLINE {
       constexpr int BUF = decltype(parity)::value;
       advance(stage);
       step(s_k[BUF], stage * kStageRows - 32, s_v[BUF ^ 1]);

@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
   // A single workgroup knows its first rows before it knows the length: their page numbers come beside it.
   // Page numbers of a block, from the list alone; rows behind the end are the last one again, and a page that is not in the pool is page 0
   // (they weigh nothing).
-  auto fetch_ids = [&](int block, int slot) { dma_4(list + (min(block * 32 + m, a.n_rows - 1) >> a.lists.shift), s_ids[wave][slot]); };
+  auto fetch_ids = [&](int block, int slot) CKV_INLINE { dma_4(list + (min(block * 32 + m, a.n_rows - 1) >> a.lists.shift), s_ids[wave][slot]); };
   if (single) {
     fetch_ids(wave, 0);
     fetch_ids(wave + WAVES, 1);
@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
   u32x4_d qf[I::STEPS];
   load_query<DT, DH>(a, b, c, valid, half, qf);
   char *k_rows = s_rows[wave], *v_rows = s_rows[wave] + BLOCK;
-  auto find_rows = [&](int block, int slot) {  // returns which of the 32 are on no page
+  auto find_rows = [&](int block, int slot) CKV_INLINE {  // returns which of the 32 are on no page
     const int at = min(m, range.end - 1 - block * 32);
     const int id = s_ids[wave][slot][at], row = (block * 32 + at) & ((1 << a.lists.shift) - 1);
     const bool ok = (unsigned)id < (unsigned)a.lists.n_pages;
@@ -64,14 +64,14 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
     wait_lds_reads();
     return missing;
   };
-  auto fetch_k = [&]() {
+  auto fetch_k = [&]() CKV_INLINE {
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       const int row = j * I::ROWS_PER_LOAD + lane / I::PIECES;
       dma_16<STREAM>(kb + s_at[wave][row].k + I::k_piece(row, lane % I::PIECES) * 16, k_rows + 1024 * j);
     }
   };
-  auto fetch_v = [&]() {
+  auto fetch_v = [&]() CKV_INLINE {
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       const int row = j * I::ROWS_PER_LOAD + lane / I::PIECES;
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
 
   Running run;
   f32x16_p acc[I::DTILES];
-  auto sweep = [&](auto careful, int mode) {
+  auto sweep = [&](auto careful, int mode) CKV_INLINE {
     constexpr bool CAREFUL = decltype(careful)::value;
     run = none_yet();
 #pragma unroll

@@ -6,6 +6,9 @@
 
 namespace ckv {
 
+// For lambdas: one that is called from several places may stay a function, and all it refers to lies in memory then.
+#define CKV_INLINE __attribute__((always_inline))
+
 struct PageLists {
   const int32_t *table, *length, *count;  // count may be null: all n new rows
   int64_t table_b, table_h;               // entries between batch elements, between KV heads

@@ -11,6 +11,8 @@
 //
 // Angles: position * inv_freq / (2 pi) in fp64, off by less than 2^-51 of itself (2^-31 of a turn a million turns away), and without
 // its whole turns to fp32.
+#include <type_traits>
+
 #include "ckv_pages.h"
 
 namespace ckv {
@@ -30,35 +32,37 @@ struct RowsArgs {
   int heads;                       // KV heads of a workgroup (grid.y of them)
 };
 
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_r;
+
 constexpr int kRowThreads = 256;
 constexpr int kMostTokens = 8;     // tokens of a workgroup
 constexpr int kMostHeads = kRowThreads / kMostTokens;  // KV heads: a thread for every (token, head)
 
-// Four components as fp32, and back: to the nearest, ties to even, the one rounding of a row's way.
+// Four components as they lie in memory; as fp32; and back: to the nearest, ties to even, the one rounding of a row's way.
 template <int DT>
-__device__ __forceinline__ void load_four(const char *p, float *x) {
-  if (DT == CKV_BF16) {
-    const uint2 raw = *reinterpret_cast<const uint2 *>(p);
-    x[0] = __uint_as_float(raw.x << 16);
-    x[1] = __uint_as_float(raw.x & 0xffff0000u);
-    x[2] = __uint_as_float(raw.y << 16);
-    x[3] = __uint_as_float(raw.y & 0xffff0000u);
-  } else {
-    const uint4 raw = *reinterpret_cast<const uint4 *>(p);
-    x[0] = __uint_as_float(raw.x);
-    x[1] = __uint_as_float(raw.y);
-    x[2] = __uint_as_float(raw.z);
-    x[3] = __uint_as_float(raw.w);
-  }
+struct Four {
+  typedef typename std::conditional<DT == CKV_BF16, u32x2_r, u32x4_d>::type raw_t;
+};
+template <int DT>
+__device__ __forceinline__ typename Four<DT>::raw_t load_four(const char *p) {
+  return *reinterpret_cast<const typename Four<DT>::raw_t *>(p);
 }
 template <int DT>
-__device__ __forceinline__ void store_four(char *p, const float *x) {
-  if (DT == CKV_BF16) {
-    *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+__device__ __forceinline__ void to_floats(const typename Four<DT>::raw_t &raw, float *x) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    x[e] = __uint_as_float(DT != CKV_BF16 ? raw[DT != CKV_BF16 ? e : 0] : e % 2 ? raw[e / 2] & 0xffff0000u : raw[e / 2] << 16);
+}
+template <int DT>
+__device__ __forceinline__ typename Four<DT>::raw_t from_floats(const float *x) {
+  typename Four<DT>::raw_t raw;
+  if constexpr (DT == CKV_BF16) {
+    raw = u32x2_r{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
   } else {
-    *reinterpret_cast<uint4 *>(p) =
-        make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) raw[e] = __float_as_uint(x[e]);
   }
+  return raw;
 }
 
 enum RowForm { kCopied, kHalves, kNeighbours };  // what happens to keys and queries: nothing, or norm and rotation in these pairs
@@ -66,20 +70,22 @@ enum RowForm { kCopied, kHalves, kNeighbours };  // what happens to keys and que
 // Eight components of a row in a lane, at `at0` and `at1` bytes (four each), or as they are.
 template <int DT, int DH, int FORM>
 struct LaneRow {
-  static constexpr int ESIZE = DT == CKV_BF16 ? 2 : 4, LPR = DH / 8;
   static constexpr bool NEIGHBOURS = FORM == kNeighbours;
-  float x[8];
+  typename Four<DT>::raw_t lo, hi;
   __device__ __forceinline__ void load(const char *row, int at0, int at1) {
-    load_four<DT>(row + at0, &x[0]);
-    load_four<DT>(row + at1, &x[4]);
+    lo = load_four<DT>(row + at0);
+    hi = load_four<DT>(row + at1);
   }
   // all lanes of the row take part
   __device__ __forceinline__ void change(bool norm, float eps, const float (&w)[8], bool turned, const float2 (&turn)[4]) {
+    float x[8];
+    to_floats<DT>(lo, &x[0]);
+    to_floats<DT>(hi, &x[4]);
     if (norm) {
       float sq = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) sq = fmaf(x[e], x[e], sq);
-      sq = row_sum<LPR>(sq);
+      sq = row_sum<DH / 8>(sq);
       const float f = __builtin_amdgcn_rsqf(fmaf(sq, 1.0f / DH, eps));  // one unit of the last place
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = x[e] * f * w[e];
@@ -94,10 +100,12 @@ struct LaneRow {
         p2 = y2 * turn[e].x + y * turn[e].y;
       }
     }
+    lo = from_floats<DT>(&x[0]);
+    hi = from_floats<DT>(&x[4]);
   }
   __device__ __forceinline__ void store(char *row, int at0, int at1) const {
-    store_four<DT>(row + at0, &x[0]);
-    store_four<DT>(row + at1, &x[4]);
+    *reinterpret_cast<typename Four<DT>::raw_t *>(row + at0) = lo;
+    *reinterpret_cast<typename Four<DT>::raw_t *>(row + at1) = hi;
   }
 };
 template <int DT, int DH>
@@ -178,48 +186,73 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(RowsArgs a) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) qw[e] = kw[e] = 1.0f;
   if (TRANSFORM && a.norm && a.q_weight) {
-    load_four<DT>(static_cast<const char *>(a.q_weight) + at0, &qw[0]);
-    load_four<DT>(static_cast<const char *>(a.q_weight) + at1, &qw[4]);
+    to_floats<DT>(load_four<DT>(static_cast<const char *>(a.q_weight) + at0), &qw[0]);
+    to_floats<DT>(load_four<DT>(static_cast<const char *>(a.q_weight) + at1), &qw[4]);
   }
   if (TRANSFORM && a.norm && a.k_weight) {
-    load_four<DT>(static_cast<const char *>(a.k_weight) + at0, &kw[0]);
-    load_four<DT>(static_cast<const char *>(a.k_weight) + at1, &kw[4]);
+    to_floats<DT>(load_four<DT>(static_cast<const char *>(a.k_weight) + at0), &kw[0]);
+    to_floats<DT>(load_four<DT>(static_cast<const char *>(a.k_weight) + at1), &kw[4]);
   }
 
-  for (int i = slot; i < ways; i += ABREAST) {
-    const Way &w = s_way[i];
-    if (!w.here) continue;  // a row's lanes all go on or none does
+  // A (token, KV head)'s rows.
+  struct Rows {
     LaneRow<DT, DH, FORM> key, query[Q];
     LaneRow<DT, DH, kCopied> value;
+  };
+  const int queries = a.q ? a.G : 0;
+  auto load = [&](Rows &rows, int i) CKV_INLINE {
+    if (i >= ways || !s_way[i].here) return;
+    const Way &w = s_way[i];
+    if (a.k) rows.key.load(a.k + w.k, at0, at1);
+    if (PAGED) rows.value.load(a.v + w.v, 8 * sub * ESIZE, 0);
     const char *from = a.q + w.q;
-    char *to = a.q_out + w.q_out;
-    const int64_t to_step = (int64_t)a.n * ROW;
-    if (a.k) key.load(a.k + w.k, at0, at1);
-    if (PAGED) value.load(a.v + w.v, 8 * sub * ESIZE, 0);
-    const int queries = a.q ? a.G : 0;
 #pragma unroll
     for (int h = 0; h < Q; ++h)
-      if (h < queries) query[h].load(from + h * a.qs[1], at0, at1);
+      if (h < queries) rows.query[h].load(from + h * a.qs[1], at0, at1);
+  };
+  auto finish = [&](Rows &rows, int i) CKV_INLINE {
+    const Way &w = s_way[i];
+    if (!w.here) return;  // a row's lanes all go on or none does
+    const int64_t to_step = (int64_t)a.n * ROW;
+    const char *from = a.q + w.q;
+    char *to = a.q_out + w.q_out;
     float2 turn[4];
     if (turned) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) turn[e] = s_turn[i % a.tokens][4 * sub + e];
     }
     if (a.k) {
-      key.change(a.norm, a.eps, kw, turned, turn);
-      if (w.placed) key.store(a.k_out + w.k_out, at0, at1);
+      rows.key.change(a.norm, a.eps, kw, turned, turn);
+      if (w.placed) rows.key.store(a.k_out + w.k_out, at0, at1);
     }
-    if (PAGED && w.placed) value.store(a.v_out + w.v_out, 8 * sub * ESIZE, 0);
+    if (PAGED && w.placed) rows.value.store(a.v_out + w.v_out, 8 * sub * ESIZE, 0);
     for (int h0 = 0; h0 < queries; h0 += Q) {
 #pragma unroll
       for (int h = 0; h < Q; ++h) {
         if (h0 + h < queries) {
-          query[h].change(a.norm, a.eps, qw, turned, turn);
-          query[h].store(to + (h0 + h) * to_step, at0, at1);
-          if (h0 + Q + h < queries) query[h].load(from + (h0 + Q + h) * a.qs[1], at0, at1);
+          rows.query[h].change(a.norm, a.eps, qw, turned, turn);
+          rows.query[h].store(to + (h0 + h) * to_step, at0, at1);
+          if (h0 + Q + h < queries) rows.query[h].load(from + (h0 + Q + h) * a.qs[1], at0, at1);
         }
       }
     }
+  };
+  // Dense bf16 rows: the next (token, KV head)'s are on their way while these are worked on (a 32k prompt 145 -> 137 us). Into pages, and
+  // in f32, the registers that this takes cost more than it brings (a chunk of 4k tokens 46.5 -> 49.9).
+  constexpr bool AHEAD = !PAGED && DT == CKV_BF16;
+  Rows even, odd;
+  if (AHEAD) load(even, slot);
+  for (int i = slot; i < ways; i += (AHEAD ? 2 : 1) * ABREAST) {
+    if (!AHEAD) {
+      load(even, i);
+      finish(even, i);
+      continue;
+    }
+    load(odd, i + ABREAST);
+    finish(even, i);
+    if (i + ABREAST >= ways) break;
+    load(even, i + 2 * ABREAST);
+    finish(odd, i + ABREAST);
   }
 }
 
