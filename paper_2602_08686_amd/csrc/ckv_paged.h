@@ -326,7 +326,10 @@ __device__ __forceinline__ void store_lse(const PagedArgs &a, int b, const Colum
 }
 
 constexpr int kRowsCols = 32;  // columns of a tile of paged_rows_kernel
-constexpr int kMostRowsCols = 64;  // up to here it takes a call's columns, in two tiles that read the same rows at the same time
+// Up to here it takes a call's columns, in tiles that read the same rows at the same time. bf16: two tiles (35 columns, 9k rows: 41 us with
+// paged_tile_kernel, 37; from three tiles on that one reads less). f32, where the products of the matrix cores take longer than the rows: their
+// shares of the rows are what keeps the chip busy (200 columns, 1k rows 20.0 -> 13.1, 256, 2k 37 -> 34, 2048, 4k the other way round).
+constexpr int kMostRowsCols = 64, kMostRowsColsF32 = 256;
 void launch_paged_rows(const PagedArgs &a, bool bf16, int d, hipStream_t stream);
 
 }  // namespace ckv

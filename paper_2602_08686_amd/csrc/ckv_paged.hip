@@ -356,7 +356,7 @@ PagedPlan plan_paged(const Shape &s, int n_rows) {
   PagedPlan p;
   const bool bf16 = s.esize == 2;
   const int64_t units = (int64_t)s.Bz * s.Hkv, cols = (int64_t)s.G * s.T;
-  p.by_rows = cols <= kMostRowsCols;
+  p.by_rows = cols <= (bf16 ? kMostRowsCols : kMostRowsColsF32);
   const int waves = units * ((cols + 255) / 256) >= kComputeUnits ? 8 : 4;
   p.tile_cols = p.by_rows ? kRowsCols : waves * 32;
   p.stage_rows = p.by_rows ? 32 : kStageRows;
