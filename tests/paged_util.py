@@ -168,6 +168,23 @@ def attention(c, s):
         there = np.array([r is not None for r in rows], bool)
         at = np.array([r if r is not None else (0, 0) for r in rows], int).reshape(-1, 2)
         k, v = (values(s[m][at[:, 0], h0, at[:, 1]]).astype(np.float64) for m in ("k_pages", "v_pages"))
+        if count and len(rows) and there.all() and length >= count and np.isfinite(k).all() and np.isfinite(v).all():
+            # nothing out of the ordinary: all tokens of a head at once
+            seen = np.arange(len(rows)) <= (length - count + np.arange(count))[:, None]
+            for h in range(g * G, (g + 1) * G):
+                q = values(s["q"])[b, h, :count].astype(np.float64)
+                z = np.where(seen, scale * (q @ k.T), -np.inf)
+                top = z.max(1, keepdims=True)
+                w = np.exp(z - top)
+                total = w.sum(1, keepdims=True)
+                w /= total
+                lse[b, h, :count], out[b, h, :count] = (top + np.log(total))[:, 0], w @ v
+                e = (d + 4) * H24 * scale * np.where(seen, np.abs(q) @ np.abs(k).T, 0.0).max(1)
+                many = seen.sum(1) + 16
+                lse_tol[b, h, :count] = e + many * H24 + 2 * H24 * np.abs(lse[b, h, :count])
+                out_tol[b, h, :count] = ((2 * e + many * 2 * H24 + (H8 if bf16 else 0.0))[:, None] * (w @ np.abs(v))
+                                         + (H8 if bf16 else H24) * np.abs(out[b, h, :count]))
+            continue
         for h in range(g * G, (g + 1) * G):
             for i in range(count):
                 sees = there & (np.arange(len(rows)) <= length - count + i)
@@ -210,6 +227,8 @@ ROWS = [
     case(dtype="f32", heads=(2, 2), n=5, lengths=((5, 5),), page=2, pool_token_major=True),
     case(d=64, heads=(6, 3), n=33, lengths=((1000, 1000, 1000),), rot_dim=48, page=256),
     case(heads=(8, 2), n=4, lengths=((2, 9), (-3, 4)), counts=((4, 9), (4, -1)), rot_dim=128, page=4),  # rows before the list, odd counts
+    case(d=64, heads=(40, 40), n=2, lengths=((2,) * 40,), norm=True, rot_dim=64, pairing=N, page=2),     # more heads than a workgroup takes
+    case(heads=(18, 2), n=3, lengths=((3, 3),), norm=True, rot_dim=64, page=8, token_major=False),       # more queries than are in flight together
 ]
 
 ATTEND = [
@@ -225,4 +244,6 @@ ATTEND = [
     case(dtype="f32", n=9, heads=(2, 1), lengths=((200,), (64,)), counts=((9,), (2,)), page=16, scale=0.2),
     case(n=1, heads=(4, 1), lengths=((2500,),), page=16),                             # several workgroups along the rows
     case(n=3, heads=(2, 1), d=64, lengths=((1500,), (64,)), page=32, n_rows=1400),      # a bound below the length
+    case(dtype="f32", n=260, heads=(1, 1), d=64, lengths=((270,),), page=16),            # f32 beyond the columns that share rows
+    case(n=40, heads=(3, 1), d=64, lengths=((45,), (40,)), counts=((40,), (0,)), page=16),  # a sequence without new tokens
 ]

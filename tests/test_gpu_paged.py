@@ -102,6 +102,9 @@ LONG = [
     u.case(n=257, heads=(4, 1), lengths=((700,),), page=32),
     u.case(n=300, heads=(2, 2), d=64, lengths=((300, 300), (555, 411)), counts=((300, 300), (1, 1)), page=256),
     u.case(n=520, heads=(1, 1), lengths=((1500,),), page=16),
+    u.case(n=66, heads=(64, 64), d=64, lengths=(tuple(range(66, 130)),) * 4, page=16, by_head=True),    # tiles of eight waves
+    u.case(n=17, heads=(32, 8), lengths=tuple((17 + 31 * b,) * 8 for b in range(32)), page=32),
+    u.case(n=600, heads=(8, 8), d=64, lengths=((600,) * 8,) * 8, counts=((600,) * 8,) * 7 + ((5,) * 8,), page=64),
     u.case(dtype="f32", n=1, heads=(8, 2), lengths=((5000, 30),), page=16),
     u.case(dtype="f32", n=130, heads=(2, 1), d=64, lengths=((900,),), page=64),
     u.case(dtype="f32", n=20, heads=(6, 2), lengths=((2100, 40),), by_head=True, page=1),
@@ -156,6 +159,63 @@ def test_what_is_not_seen_has_no_influence(c, kind):
     out, lse = attend(c, t)
     torch.cuda.synchronize()
     check_attention(c, s, out, lse)
+
+
+def test_queries_or_keys_alone_and_slices_of_one_projection():
+    """q, k and v as slices of what one projection leaves (token by token, their heads side by side), queries alone, keys alone."""
+    c = u.case(n=5, heads=(6, 2), lengths=((9, 9), (40, 40)), norm=True, rot_dim=32, page=8)
+    s = u.make(c)
+    d, n = c["d"], c["n"]
+    fused = torch.zeros(2, n, 10 * d + 64, dtype=torch.bfloat16, device=DEV)
+    part = {"q": fused[..., :6 * d].unflatten(-1, (6, d)), "k": fused[..., 6 * d:8 * d].unflatten(-1, (2, d)), "v": fused[..., 8 * d:10 * d].unflatten(-1, (2, d))}
+    part = {m: x.transpose(1, 2) for m, x in part.items()}
+    for m, x in part.items():
+        x.copy_(gpu(s[m]))
+    t, rot = on_gpu(c, s), u.rotation(c)
+    for m in ("q", "k"):
+        p = B.step_params(**{m: part[m]}, n_q_heads=6, n_kv_heads=2)
+        out = nines(c, part[m].shape[1])
+        q, k = (part[m], None) if m == "q" else (None, part[m])
+        B.ckv_norm_rotate(p, rot, q, k, t["positions"], t["inv_freq"], t["q_weight"], t["k_weight"], out if q is not None else None,
+                          out if k is not None else None)
+        torch.cuda.synchronize()
+        want, tol = u.transform(c, s, s[m], s[m + "_weight"])
+        u.check(host(out), want, tol, m)
+    p = B.step_params(**part, n_q_heads=6, n_kv_heads=2)
+    B.ckv_paged_append(p, rot, t["pages"], part["k"], part["v"], t["k_pages"], t["v_pages"], t["table"], t["length"], positions=t["positions"],
+                       inv_freq=t["inv_freq"], k_weight=t["k_weight"])
+    torch.cuda.synchronize()
+    kp, kt, vp = u.appended(c, s)
+    u.check(host(t["k_pages_all"]), kp, kt, "k_pages")
+    u.check(host(t["v_pages_all"]), vp, np.zeros_like(vp), "v_pages")
+    out, lse = nines(c, 6), torch.full((2, 6, n), 9.0, device=DEV)
+    B.ckv_paged_attention(p, t["pages"], part["q"], t["k_pages"], t["v_pages"], t["table"], t["length"], t["n_rows"], out, lse, t["ws"])
+    torch.cuda.synchronize()
+    check_attention(c, dict(s, **{m: u.stored(host(t[m + "_all"]), "bf16") for m in ("k_pages", "v_pages")}), out, lse)
+
+
+def test_pages_that_two_lists_share():
+    """Two sequences with a common beginning: the same pages in both lists, pages of their own behind."""
+    c = u.case(n=3, heads=(4, 2), lengths=((70, 70), (90, 90)), page=16)
+    s = u.make(c)
+    s["table"][1, :4] = s["table"][0, :4]
+    t = on_gpu(c, s)
+    out, lse = attend(c, t)
+    torch.cuda.synchronize()
+    check_attention(c, s, out, lse)
+
+
+def test_a_bound_far_above_the_lengths():
+    """A call that was planned for long lists (a graph, say) on short ones, down to none: shared out, merged and empty all the same."""
+    for lengths in (((40, 40),), ((1, 1),), ((0, 0),), ((700, 2),)):
+        c = u.case(n=2, heads=(8, 2), lengths=lengths, counts=(tuple(min(2, x) for x in lengths[0]),), page=16)
+        s = u.make(c)
+        s["table"] = np.concatenate([s["table"], np.full((1, 4000 - s["table"].shape[1]), -1, np.int32)], 1)
+        t = on_gpu(c, s)
+        assert t["n_rows"] == 64000 and t["ws"] is not None
+        out, lse = attend(c, t)
+        torch.cuda.synchronize()
+        check_attention(c, s, out, lse)
 
 
 def test_lists_far_apart_in_a_large_pool():
