@@ -20,8 +20,11 @@ struct PagedArgs {
   float2 *stats;       // [unit][column tile][chunk][column of the tile]: running maximum (log2), sum
   int Hq, Hkv, G, n, n_rows;
   int tile_cols, col_tiles, stage_rows, n_chunks, workgroups;  // of the plan
+  tag_t *marks;        // [unit][column tile][chunk] or null: who finds a tile's marks complete joins its chunks, no kernel behind this one
+  tag_t tag;           // of the launch
   float scale2;        // softmax scale * log2(e)
 };
+constexpr int kMostChunks = 64;  // a lane for each
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_p;
 typedef __attribute__((ext_vector_type(16))) float f32x16_p;
@@ -330,6 +333,11 @@ constexpr int kRowsCols = 32;  // columns of a tile of paged_rows_kernel
 // paged_tile_kernel, 37; from three tiles on that one reads less). f32, where the products of the matrix cores take longer than the rows: their
 // shares of the rows are what keeps the chip busy (200 columns, 1k rows 20.0 -> 13.1, 256, 2k 37 -> 34, 2048, 4k the other way round).
 constexpr int kMostRowsCols = 64, kMostRowsColsF32 = 256;
+// Columns of a tile times chunks up to which a tile's chunks are joined in the launch that makes them: above, one workgroup takes longer
+// with them than a kernel of many behind this one. us, two launches / one: one token, 32/8 heads, 2000 rows 12.7 / 11.7 (4 x 8), batch 4 14.5 / 13.6,
+// 32768 rows, batch 4 87.1 / 85.8, 65000 rows 50.5 / 49.8 (4 x 32); 35 columns, 9001 rows 36.1 / 36.4 (32 x 8), f32, 256 columns 34.2 / 37.0. (A
+// counter instead of the marks: 65000 rows 93, its 32 workgroups one behind the other.)
+constexpr int kMostJoined = 128;
 void launch_paged_rows(const PagedArgs &a, bool bf16, int d, hipStream_t stream);
 
 }  // namespace ckv

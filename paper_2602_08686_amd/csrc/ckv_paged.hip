@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
 
 // Chunks of a column, in their order. A column's lanes take four components each, and for the weights a chunk each; loads of eight chunks are in flight
 // together (one after the other, sixteen chunks took 12 us, now 5).
-constexpr int kMergeThreads = 256, kMostChunks = 64;
+constexpr int kMergeThreads = 256;
 template <int DT, int DH>
 __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a) {
   constexpr int PIECES = DH / 4, COLS = kMergeThreads / PIECES, SHARE = kMostChunks / PIECES;
@@ -370,7 +370,8 @@ PagedPlan plan_paged(const Shape &s, int n_rows) {
   if (chunks < 1) chunks = 1;
   p.n_chunks = (int)chunks;
   p.workgroups = tiles * chunks;
-  p.workspace_bytes = chunks == 1 ? 0 : (size_t)p.workgroups * p.tile_cols * (s.d + 2) * sizeof(float);
+  p.joined = p.by_rows && (cols < kRowsCols ? cols : kRowsCols) * chunks <= kMostJoined;
+  p.workspace_bytes = chunks == 1 ? 0 : (size_t)p.workgroups * p.tile_cols * (s.d + 2) * sizeof(float) + (p.joined ? p.workgroups * sizeof(tag_t) : 0);
   return p;
 }
 
@@ -384,7 +385,7 @@ static void launch_paged_of(const PagedArgs &a, const PagedPlan &plan, int units
   if (plan.by_rows) launch_paged_rows(a, DT == CKV_BF16, DH, stream);
   else if (plan.tile_cols == 256) launch_tiles<DT, DH, 8>(a, stream);
   else launch_tiles<DT, DH, 4>(a, stream);
-  if (plan.n_chunks > 1) {
+  if (plan.n_chunks > 1 && !plan.joined) {
     constexpr int COLS = kMergeThreads / (DH / 4);
     const unsigned blocks = (unsigned)(a.G * a.n + COLS - 1) / COLS;
     hipLaunchKernelGGL((paged_merge_kernel<DT, DH>), dim3(units * blocks), dim3(kMergeThreads), 0, stream, a);
@@ -427,6 +428,8 @@ hipError_t launch_paged_attention(const ckv_params *p, const Shape &s, const Pag
   a.lse = lse;
   a.part = reinterpret_cast<float *>(ws);
   a.stats = reinterpret_cast<float2 *>(a.part + (plan.n_chunks > 1 ? (size_t)plan.workgroups * plan.tile_cols * s.d : 0));
+  a.marks = plan.n_chunks > 1 && plan.joined ? reinterpret_cast<tag_t *>(a.stats + plan.workgroups * plan.tile_cols) : nullptr;
+  a.tag = a.marks ? launch_tag() : 0;
   a.Hq = s.Hq; a.Hkv = s.Hkv; a.G = s.G;
   a.n = s.T;
   a.n_rows = n_rows;

@@ -5,7 +5,11 @@
 // loads go straight to LDS. K's place is free once the first product has read it and V's once the second has, so the next
 // 32 rows' K is on its way during the softmax and the second product, their V during the next first product. Page numbers
 // come the same way, one block further ahead; a lane per row turns them into offsets.
-// Waves are joined in LDS in wave order, chunks by paged_merge_kernel in chunk order.
+// Waves are joined in LDS in wave order, chunks in chunk order: by paged_merge_kernel, or where their sums are few in this launch. Each workgroup
+// then leaves its sums, past its own caches, and behind them a mark, the launch's tag (another value for every launch, which undefined memory
+// does not hold), and looks at the marks of its tile. Who finds all of them, which the last one to mark does unless somebody else has before,
+// joins the chunks and takes the marks back, as a replay of the launch has the same tag. Nobody waits for anybody; two that find them
+// all write the same values.
 #include "ckv_paged.h"
 
 namespace ckv {
@@ -23,6 +27,8 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
   };
   __shared__ Offsets s_at[WAVES][32];
   __shared__ float2 s_stats[WAVES][32];
+  __shared__ int s_last;
+  static_assert(32 * kMostChunks * sizeof(float2) <= sizeof(s_rows), "the chunks' sums are joined there too");
   static_assert(32 * DH * 4 <= 2 * BLOCK, "a wave's sums take its rows' place");
 
   // a list's column tiles, which read the same rows, one behind the other
@@ -43,7 +49,9 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
   }
   const TileRange range = tile_range(a, unit, tile);
   const int first = chunk * range.per_chunk, last = min(first + range.per_chunk, range.stages);  // blocks of 32 rows
-  if (range.cols <= 0 || (first >= last && !single)) {  // the merge reads the chunks that have blocks
+  const int used = (range.stages + range.per_chunk - 1) / range.per_chunk;  // chunks that have blocks, which are what the merge reads
+  const bool alone = single || (a.marks && used <= 1);
+  if (range.cols <= 0 || (first >= last && !(alone && chunk == 0))) {
     wait_vm_at_most<0>();
     return;
   }
@@ -164,15 +172,66 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
       sum = fmaf(st.y, f, sum);
       num = add_part(num, *reinterpret_cast<const f32x4_p *>(s_rows[w] + local * DH * 4 + ((piece ^ local) % PIECES) * 16), f);
     }
-    if (single) {
+    if (alone) {
       const Column o = column(a, unit, tile, local);
       store_out<DT>(out_row(a, b, o), 4 * piece, num * inverse_sum(sum));
       if (piece == 0) store_lse(a, b, o, top, sum);
     } else {
-      *reinterpret_cast<f32x4_p *>(a.part + (row0 + local) * DH + 4 * piece) = num;
-      if (piece == 0) a.stats[row0 + local] = make_float2(top, sum);
+      uint64_t *to = reinterpret_cast<uint64_t *>(a.part + (row0 + local) * DH + 4 * piece);
+      store_across(to, __builtin_bit_cast(uint64_t, make_float2(num[0], num[1])));
+      store_across(to + 1, __builtin_bit_cast(uint64_t, make_float2(num[2], num[3])));
+      if (piece == 0) store_across(reinterpret_cast<uint64_t *>(a.stats + row0 + local), __builtin_bit_cast(uint64_t, make_float2(top, sum)));
     }
   }
+  if (alone || !a.marks) return;
+
+  wait_vm_at_most<0>();  // what this lane left has arrived
+  __syncthreads();
+  tag_t *marks = a.marks + ((size_t)unit * a.col_tiles + tile) * a.n_chunks;
+  if (wave == 0) {
+    if (lane == 0) store_across(marks + chunk, a.tag);
+    wait_vm_at_most<0>();
+    const bool missing = lane < used && load_across(marks + lane) != a.tag;
+    if (lane == 0) s_last = 1;
+    if (__any(missing)) s_last = 0;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  const size_t tile0 = row0 - (size_t)chunk * kRowsCols;
+  float2 *stats = reinterpret_cast<float2 *>(s_rows);  // [column][chunk]
+  for (int i = threadIdx.x; i < range.cols * used; i += WAVES * kWave) {
+    const int local = i / used, c = i % used;
+    stats[i] = __builtin_bit_cast(float2, load_across(reinterpret_cast<const uint64_t *>(a.stats + tile0 + (size_t)c * kRowsCols + local)));
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < range.cols * PIECES; i += WAVES * kWave) {
+    const int local = i / PIECES, piece = i % PIECES;
+    const float2 *st = stats + local * used;
+    float top = st[0].x, sum = 0.0f;
+    for (int c = 1; c < used; ++c) top = fmaxf(top, st[c].x);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    const uint64_t *from = reinterpret_cast<const uint64_t *>(a.part + (tile0 + local) * DH + 4 * piece);
+    f32x4_p num = {0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int BATCH = 8;
+    for (int c0 = 0; c0 < used; c0 += BATCH) {
+      float2 x[BATCH][2];
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) x[j][e] = __builtin_bit_cast(float2, load_across(from + (size_t)min(c0 + j, used - 1) * (kRowsCols * DH / 2) + e));
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        if (c0 + j >= used) continue;
+        const float f = __builtin_amdgcn_exp2f(st[c0 + j].x - ref);
+        sum = fmaf(st[c0 + j].y, f, sum);
+        num = add_part(num, f32x4_p{x[j][0].x, x[j][0].y, x[j][1].x, x[j][1].y}, f);
+      }
+    }
+    const Column o = column(a, unit, tile, local);
+    store_out<DT>(out_row(a, b, o), 4 * piece, num * inverse_sum(sum));
+    if (piece == 0) store_lse(a, b, o, top, sum);
+  }
+  if (wave == 0 && lane < used) store_across(marks + lane, (tag_t)0);  // a replay of this launch has the same tag
 }
 
 template <int DT, int DH, int WAVES>

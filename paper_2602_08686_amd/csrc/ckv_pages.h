@@ -46,6 +46,7 @@ struct PagedPlan {
   int col_tiles;     // such tiles of a (batch element, KV head)
   int stage_rows;    // rows of a list are shared out in multiples of this
   int n_chunks;      // workgroups along the rows of a list
+  bool joined;       // chunks are joined in the same launch
   int64_t workgroups;
   size_t workspace_bytes;
 };

@@ -305,6 +305,47 @@ def test_calls_on_several_streams_and_from_a_graph(c):
         (t["out"].float().sum() + t["lse"].sum()).item()
 
 
+def test_a_graph_on_growing_lists():
+    """A decoding step captured once, its lengths counted on between the replays: from an empty list over one chunk's rows to several."""
+    Bz, Hq, Hkv, d, page, cap = 2, 8, 2, 128, 16, 8192
+    g = torch.Generator(device=DEV).manual_seed(9)
+    kp, vp = (torch.randn(Bz * cap // page, Hkv, page, d, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    ids = torch.randperm(Bz * cap // page, generator=g, device=DEV).to(torch.int32).view(Bz, -1)
+    q = torch.randn(Bz, Hq, 1, d, generator=g, device=DEV).to(torch.bfloat16)
+    p, pages = B.step_params(q=q, n_q_heads=Hq, n_kv_heads=Hkv), B.pages_for(kp, vp, ids)
+    length, out, lse = torch.zeros(Bz, Hkv, dtype=torch.int32, device=DEV), torch.empty_like(q), torch.empty(Bz, Hq, 1, device=DEV)
+    need = B.ckv_paged_workspace_bytes(p, cap)
+    ws = [torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    call = lambda o, l, w: B.ckv_paged_attention(p, pages, q, kp, vp, ids, length, cap, o, l, w)  # noqa: E731
+    call(out, lse, ws[0])
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):   # two graphs that share a workspace, replayed in turn
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(out, lse, ws[0])
+        graphs.append(graph)
+    for i, n in enumerate((0, 1, 31, 33, 300, 1025, 2047, 5000, 8192, 64, 8191)):
+        length.fill_(n)
+        length[0, 1] = max(n - 7, 0)
+        out.fill_(9.0)
+        o, l = torch.empty_like(out), torch.empty_like(lse)
+        torch.cuda.synchronize()
+        graphs[i % 2].replay()
+        call(o, l, ws[1])
+        torch.cuda.synchronize()
+        assert torch.equal(out, o) and torch.equal(lse, l), n
+        for b, h in ((0, 0), (0, 7), (1, 4)):
+            m = int(length[b, h // 4])
+            rows = torch.arange(m, device=DEV)
+            k, v = (t[ids[b, rows // page].long(), h // 4, rows % page].double() for t in (kp, vp))
+            z = k @ q[b, h, 0].double() / d ** 0.5
+            assert m == 0 and float(l[b, h, 0]) == -float("inf") or abs(float(l[b, h, 0]) - float(torch.logsumexp(z, 0))) < 2e-5
+            w = torch.softmax(z, 0)
+            ref, size = w @ v, w @ v.abs()
+            assert ((o[b, h, 0].double() - ref).abs() <= 2.0 ** -8 * (size + ref.abs()) + 1e-4 * size).all()
+
+
 def test_a_prompt_through_all_of_it():
     """Two prompts in chunks: rows into pages, attention of each chunk, and beside it dense keys for the retention step, which takes the last
     window's lse from the attention; the kept rows move into lists that differ by head, and tokens are decoded over them."""
