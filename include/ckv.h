@@ -382,7 +382,7 @@ ckv_status ckv_discarded_mass(const ckv_params *params, int32_t n_q, const float
  *   table   in  int32 page numbers at table_stride over (batch, KV head), max_pages in a row. A page number outside [0, n_pages),
  *               or a row outside [0, max_pages * page_rows): nothing is written there, and attention does not see the row.
  * A page may be in several lists (a shared prefix) as long as no call appends to it for two of them. Appending and reading are calls in
- * stream order.
+ * stream order. Outputs overlap no input of their call.
  */
 typedef struct {
   int32_t page_rows;       /* rows of a page, a power of two, 1 .. 65536                            */
@@ -402,8 +402,8 @@ typedef enum { CKV_PAIR_HALVES = 0, CKV_PAIR_NEIGHBOURS = 1 } ckv_pairing;
  * then the first rot_dim components turn by the angles a_i = position * inv_freq[i], i < rot_dim / 2, in pairs
  *     (y_i, y_{i + rot_dim/2}) (CKV_PAIR_HALVES) or (y_{2i}, y_{2i+1}) (CKV_PAIR_NEIGHBOURS):
  *     (y, y') -> (y cos a - y' sin a, y' cos a + y sin a).
- * Sums and products are fp32, angles fp64 reduced to a turn; one rounding to the type at the end. With norm = 0 and rot_dim = 0
- * rows are copied bit for bit.
+ * Sums and products are fp32 (mean square + norm_eps has to be a normal fp32 number), angles fp64 reduced to a turn; one rounding to the
+ * type at the end. With norm = 0 and rot_dim = 0 rows are copied bit for bit.
  */
 typedef struct {
   int32_t rot_dim;   /* 0 .. head_dim, a multiple of 8                                              */
@@ -452,8 +452,8 @@ ckv_status ckv_paged_append(const ckv_params *params, const ckv_rotation *rotati
  * ckv_window_scores, lse of two caches is what ckv_discarded_mass takes.
  *   n_rows      no list is longer, 1 .. max_pages * page_rows and at most 2^24; a bound near the lengths lets the call share its work out well
  *   q           in   [Bz,Hq,n,d] via q_stride
- *   out         out  [Bz,Hq,n,d] of params->dtype at element strides out_stride over (batch, query head, token), multiples of 16 bytes,
- *                    or dense (out_stride NULL)
+ *   out         out  [Bz,Hq,n,d] of params->dtype at element strides out_stride over (batch, query head, token), multiples of 16 bytes
+ *                    and each >= head_dim, or dense (out_stride NULL)
  *   lse         out  [Bz,Hq,n] fp32, natural log, or NULL
  *   workspace        ckv_paged_workspace_bytes(params, n_rows) bytes, 256-byte aligned; NULL where that is 0 (it is for refused arguments
  *                    too). Contents undefined before and after.

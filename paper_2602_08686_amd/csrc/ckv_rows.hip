@@ -9,6 +9,8 @@
 // four, neighbours in eight consecutive ones. Sums of squares cross the row's lanes as operands of the additions. Rows without
 // norm and rotation (values; keys that the retention step kept) are copied as bits.
 //
+// Measured, bf16, 32/8 heads of 128, norm and rotation: 32768 tokens 137 us, 4.9 TB/s of reads and writes, where a copy of 320 MiB reaches 5.4; up to
+// 4099 tokens of two sequences into pages, with their queries 43 us; one token of each of 16 sequences 5 us, a launch.
 // Angles: position * inv_freq / (2 pi) in fp64, off by less than 2^-51 of itself (2^-31 of a turn a million turns away), and without
 // its whole turns to fp32.
 #include <type_traits>
@@ -301,7 +303,8 @@ hipError_t launch_rows(const ckv_params *p, const Shape &s, const ckv_rotation *
   a.norm = rotation ? rotation->norm : 0;
   a.eps = rotation ? rotation->norm_eps : 0.0f;
   // Long calls: a few tokens a workgroup, so that the angles are made once for all heads. Short ones: a token's heads over several workgroups, each
-  // of which makes the angles again.
+  // of which makes the angles again. us, one token a workgroup / these: 32768 tokens 161 / 137, batch 2 of 1024 12.0 / 10.3; all heads in one / these:
+  // batch 32 of 4 tokens into pages 7.2 / 6.3.
   const int64_t tokens = (int64_t)s.Bz * s.T;
   a.tokens = 1;
   while (a.tokens < kMostTokens && 2 * a.tokens <= s.T && tokens / (2 * a.tokens) >= 4 * kComputeUnits) a.tokens *= 2;
