@@ -381,8 +381,8 @@ ckv_status ckv_discarded_mass(const ckv_params *params, int32_t n_q, const float
  *               KV head h / G.
  *   table   in  int32 page numbers at table_stride over (batch, KV head), max_pages in a row. A page number outside [0, n_pages),
  *               or a row outside [0, max_pages * page_rows): nothing is written there, and attention does not see the row.
- * A page may be in several lists (a shared prefix) as long as no call appends to it for two of them. Appending and reading are calls in
- * stream order. Outputs overlap no input of their call.
+ * A page may be in several lists (a shared prefix), or several times in one, as long as no call appends a row of it twice. Appending and
+ * reading are calls in stream order. Outputs overlap no input of their call.
  */
 typedef struct {
   int32_t page_rows;       /* rows of a page, a power of two, 1 .. 65536                            */

@@ -362,7 +362,11 @@ def ckv_paged_workspace_bytes(params, n_rows) -> int:
 def ckv_paged_attention(params, pages, q, k_pages, v_pages, table, length, n_rows, out, lse=None, workspace=None, count=None,
                         stream=None):
     """out [Bz,Hq,n,d], any strides over the first three axes."""
-    strides = None if out.is_contiguous() else (ctypes.c_int64 * 3)(*_row_strides(out, out.shape[3]))
+    strides = None
+    if not out.is_contiguous():
+        if out.dim() != 4 or out.stride(3) != 1:
+            raise ValueError("out has to be [Bz,Hq,n,d] with a contiguous last axis")
+        strides = (ctypes.c_int64 * 3)(*_row_strides(out, out.shape[3]))
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(load().ckv_paged_attention(ctypes.byref(params), ctypes.byref(pages), _at(q), _at(k_pages), _at(v_pages), _at(table),
                                       _at(length), _at(count), int(n_rows), _at(out), strides, _at(lse), _at(workspace), nbytes,

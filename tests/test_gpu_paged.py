@@ -205,6 +205,17 @@ def test_pages_that_two_lists_share():
     check_attention(c, s, out, lse)
 
 
+@pytest.mark.parametrize("n,length", [(1, 300), (3, 3000), (40, 500)])
+def test_a_page_several_times_in_a_list(n, length):
+    c = u.case(n=n, heads=(4, 2), lengths=((length, length),), page=16)
+    s = u.make(c)
+    s["table"][0, 1::2] = s["table"][0, 0]
+    t = on_gpu(c, s)
+    out, lse = attend(c, t)
+    torch.cuda.synchronize()
+    check_attention(c, s, out, lse)
+
+
 def test_a_bound_far_above_the_lengths():
     """A call that was planned for long lists (a graph, say) on short ones, down to none: shared out, merged and empty all the same."""
     for lengths in (((40, 40),), ((1, 1),), ((0, 0),), ((700, 2),)):

@@ -160,3 +160,10 @@ def test_helpers_describe_tensors():
     # one token per sequence: whatever stride torch gives the axis, the library gets one that it takes
     one = torch.zeros(2, 8, 128, dtype=torch.bfloat16)[:, :, None]
     assert B.step_params(q=one.as_strided(one.shape, (1024, 128, 1, 1)), n_q_heads=8, n_kv_heads=2).q_stride[2] == 128
+
+
+def test_an_output_without_a_contiguous_last_axis_is_refused():
+    p, pages = B.CkvParams(), B.CkvPages()
+    for out in (torch.empty(1, 4, 128, 3).transpose(2, 3), torch.empty(4, 6, 128)[:, ::2]):
+        with pytest.raises(ValueError):
+            B.ckv_paged_attention(p, pages, None, None, None, None, None, 1, out)
