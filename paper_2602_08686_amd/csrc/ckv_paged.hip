@@ -381,7 +381,7 @@ PagedPlan plan_paged(const Shape &s, int n_rows) {
   if (chunks < 1) chunks = 1;
   p.n_chunks = (int)chunks;
   p.workgroups = tiles * chunks;
-  p.joined = p.by_rows && (cols < kRowsCols ? cols : kRowsCols) * chunks <= kMostJoined;
+  p.joined = p.by_rows && cols <= kMostJoinedCols && cols * chunks <= kMostJoined;
   p.workspace_bytes = chunks == 1 ? 0 : (size_t)p.workgroups * p.tile_cols * (s.d + 2) * sizeof(float) + (p.joined ? p.workgroups * sizeof(tag_t) : 0);
   return p;
 }
