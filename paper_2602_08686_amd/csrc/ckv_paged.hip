@@ -359,9 +359,11 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a)
 // the way through memory that its sums then take, and none beside the first for so few rows that the merge would cost more than it saves.
 // Eight waves a tile once that fills the chip: 2048 new tokens, 32k rows, 32/8 heads 1062 us with four, 990 with eight, 4096 tokens over
 // themselves 162 / 151, batch 4 of 1024 tokens 59 / 56, but 512 tokens over themselves 23 / 27.
+// Of the tiles in f32 with rows of 512 bytes one fits a CU: for long lists chunks for one, 300 tokens, 8/1 heads, batch 3, 2000 rows 99 / 88, 80 tokens,
+// 8/2 heads, 20000 rows 116 / 92, 512 tokens, 32/8 heads, 4096 rows 300 / 296; but 101 tokens, 8/1 heads, batch 8, 523 rows 35 / 44.
 // Least rows of a chunk, us with half / these / twice: few columns, bf16, one token, 32/8 heads, 2000 rows 11.2 / 11.6 / 13.1, batch 4
 // 13.6 / 13.6 / 14.3; f32, 4/4 heads of 64, batch 4, 1000 rows 12.0 / 11.3 / 13.5, 200 tokens, 1024 rows 13.9 / 13.4 / 14.9; tiles, bf16, 512 tokens over
-// themselves 24.1 / 19.5 / 19.5. One chunk up to 1024 (bf16) or 256 (f32) rows of few columns: 500 rows 9.4, two chunks 10.4; batch 16,
+// themselves 24.1 / 19.5 / 19.5; f32, heads of 64, 101 tokens, 523 rows (64 / 128) 24.3 / 29.6. One chunk up to 1024 (bf16) or 256 (f32) rows of few columns: 500 rows 9.4, two chunks 10.4; batch 16,
 // 544 rows 11.2, two chunks 11.7; but batch 4 over 2000 rows 19.6 with one, 13.6 with the rule's.
 PagedPlan plan_paged(const Shape &s, int n_rows) {
   PagedPlan p;
@@ -373,8 +375,9 @@ PagedPlan plan_paged(const Shape &s, int n_rows) {
   p.stage_rows = p.by_rows ? 32 : kStageRows;
   p.col_tiles = (int)((cols + p.tile_cols - 1) / p.tile_cols);
   const int64_t tiles = units * p.col_tiles;
-  int64_t chunks = (p.by_rows || waves == 8 ? 1 : 2) * kComputeUnits / tiles;
-  const int least = p.by_rows ? (bf16 ? 256 : 128) : (bf16 ? 512 : 128);
+  const bool two = !p.by_rows && waves == 4 && (bf16 || s.d == 64 || n_rows < 1024);
+  int64_t chunks = (two ? 2 : 1) * kComputeUnits / tiles;
+  const int least = p.by_rows ? (bf16 ? 256 : 128) : bf16 ? 512 : s.d == 64 ? 64 : 128;
   const int64_t most = p.by_rows && n_rows <= (bf16 ? 1024 : 256) ? 1 : (n_rows + least - 1) / least;
   if (chunks > most) chunks = most;
   if (chunks > kMostChunks) chunks = kMostChunks;
