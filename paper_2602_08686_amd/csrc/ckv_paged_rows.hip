@@ -100,7 +100,10 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[t][r] = 0.0f;
     int block = first + wave, slot = 0;
-    if (block >= last) return;
+    if (block >= last) {
+      wait_vm_at_most<0>();  // page numbers that a single workgroup asks for ahead
+      return;
+    }
     if (!single || CAREFUL) {
       fetch_ids(block, 0);
       fetch_ids(block + WAVES, 1);

@@ -15,10 +15,16 @@ dim3 thread_idx, block_idx, block_dim, grid_dim;
 namespace {
 constexpr size_t kStack = 256 << 10;
 enum State { kRuns, kWaitsWave, kWaitsBlock, kDone };
+struct Load {
+  char *to;
+  int bytes;
+  char data[16];
+};
 struct Fiber {
   ucontext_t at;
   State state;
   int parity;
+  std::vector<Load> loads;  // not waited for yet, oldest first
 };
 struct Wave {
   alignas(64) char slot[2][64][64];
@@ -33,6 +39,10 @@ void (*hook)(int block, int barrier) = nullptr;
 
 void fiber_main() {
   (*work)();
+  if (!fibers[current].loads.empty()) {
+    fprintf(stderr, "a lane ends while its loads are in flight\n");
+    abort();
+  }
   fibers[current].state = kDone;
   swapcontext(&fibers[current].at, &scheduler);
 }
@@ -105,6 +115,19 @@ const void *exchange(const void *value, size_t bytes) {
   memcpy(w.slot[slot][lane()], value, bytes);
   wait(kWaitsWave);
   return w.slot[slot];
+}
+
+void load_later(char *to, const void *from, int bytes) {
+  Load l = {to, bytes, {}};
+  memcpy(l.data, from, bytes);
+  memset(to, 0xff, bytes);
+  fibers[current].loads.push_back(l);
+}
+void loads_at_most(size_t n) {
+  std::vector<Load> &loads = fibers[current].loads;
+  for (; loads.size() > n; loads.erase(loads.begin())) memcpy(loads[0].to, loads[0].data, loads[0].bytes);
+  const char nothing = 0;
+  exchange(&nothing, 1);
 }
 
 Pair swap_halves(uint32_t x, uint32_t y, int width) {

@@ -49,6 +49,10 @@ int lane();
 // Every live lane of the wave puts `bytes` (at most 64) down and gets the array of all 64 lanes' values (zeros for lanes
 // that have returned), valid until its next exchange.
 const void *exchange(const void *value, size_t bytes);
+// A load that may arrive any time until it is waited for: what was at `to` is gone at once, the data is there when at most n of the lane's
+// loads are left.
+void load_later(char *to, const void *from, int bytes);
+void loads_at_most(size_t n);
 uint64_t live();  // lanes of the wave that have not returned
 template <class T> T from(T x, int src) {
   T out;
