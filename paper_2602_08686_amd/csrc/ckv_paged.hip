@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
           first_product<DT, DH>(s_k[(stage - first) & 1] + k * HALF, lane, qf, z);
           hide(z, stage * kStageRows + 32 * k);
           to_weights<true>(z, a.scale2, run, mode);
-          rescale(acc, run);
+          if (mode == kFinite) rescale(acc, run);  // marks are counted, whatever the row behind them weighs
           second_product<DT, DH, true>(s_v[(stage - first) & 1] + k * HALF, lane, as_operand<DT>(z), acc, mode);
         }
       }

@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
         }
       }
       to_weights<CAREFUL>(z, a.scale2, run, mode);
-      rescale(acc, run);
+      if (!CAREFUL || mode == kFinite) rescale(acc, run);  // marks are counted, whatever the rows behind them weigh
       if (more) wait_vm_at_most<LOADS + 1>();  // V; the next page numbers and K may be on their way
       else wait_vm_at_most<0>();
       second_product<DT, DH, CAREFUL>(v_rows, lane, as_operand<DT>(z), acc, mode);

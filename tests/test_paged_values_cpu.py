@@ -1,0 +1,24 @@
+"""Attention over pages, on the host CPU, of values that are not finite or nearly so: the result is the definition's whatever the order of the rows."""
+import pytest
+
+import cpu_build as cpu
+import paged_values as pv
+from test_cpu_build import in_child, lib_path  # noqa: F401
+from test_paged_cpu import _attend, _check_attention, _fenced
+
+pytestmark = pytest.mark.skipif(cpu.CXX is None, reason="no clang++ for the host")
+
+
+def _run(path, c, make, *args):
+    lib = cpu.load(path)
+    s = _fenced(make(c, *args))
+    _check_attention(c, s, *_attend(lib, c, s))
+
+
+@pytest.mark.parametrize("near,far", [(5, 133), (5, 261), (5, 40), (70, 150), (133, 5), (150, 70)])
+@pytest.mark.parametrize("c", pv.FEW + pv.MANY, ids=range(len(pv.FEW + pv.MANY)))
+def test_what_is_seen_and_not_finite_stays(lib_path, c, near, far):  # noqa: F811
+    """A row far above in the logits does not take away an infinity or a NaN of a row before it."""
+    if far >= int(c["lengths"].min()) - c["n"]:
+        far = 100
+    in_child(_run, lib_path, c, pv.earlier, near, far, 300.0)
