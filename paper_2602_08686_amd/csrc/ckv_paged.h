@@ -16,8 +16,8 @@ struct PagedArgs {
   char *out;
   int64_t os[3];       // BYTES, as qs
   float *lse;          // [Bz][Hq][n] natural log, or null
-  float *part;         // [unit][column tile][chunk][column of the tile][d]: weighted sums of V
-  float2 *stats;       // [unit][column tile][chunk][column of the tile]: running maximum (log2), sum
+  float *part;         // [unit][column tile][chunk][column of the tile][d]: the chunk's own result, in fp32
+  float2 *stats;       // [unit][column tile][chunk][column of the tile]: reference of its weights (log2), their sum
   int Hq, Hkv, G, n, n_rows;
   int tile_cols, col_tiles, stage_rows, n_chunks, workgroups;  // of the plan
   tag_t *marks;        // [unit][column tile][chunk] or null: who finds a tile's marks complete joins its chunks, no kernel behind this one
@@ -90,6 +90,13 @@ template <class Op>
 __device__ __forceinline__ float over_halves(float x, Op op) {
   const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// Over all lanes.
+template <class Op>
+__device__ __forceinline__ float over_wave(float x, float identity, Op op) {
+  const auto bits = [=](uint32_t p, uint32_t q) { return __float_as_uint(op(__uint_as_float(p), __uint_as_float(q))); };
+  return __uint_as_float(lane_value(wave_scan(__float_as_uint(x), __float_as_uint(identity), bits), kWave - 1));
 }
 
 // A column's operand of the first product: pieces 2 s + half of its query row.
@@ -230,21 +237,24 @@ __device__ __forceinline__ void second_product(const char *image, int lane, cons
 
 // Online softmax of a lane's column: the reference of its weights (log2 domain, common to both halves of the wave; -inf before the first
 // row) and the sum of this half's weights. The reference moves only where a block's maximum outgrows it by kSlack (weights up to
-// 2^kSlack: fp32 and bf16 keep their relative precision), which it hardly ever does behind the first blocks.
+// 2^kSlack: fp32 and bf16 keep their relative precision), which it hardly ever does behind the first blocks. Weights of that size times V may be
+// beyond fp32 where their mean is not. Then there is a second sweep, and its reference lies above the maximum by so much that the weights of all
+// rows add up to less than one.
 constexpr float kSlack = 6.0f;
+__device__ __forceinline__ float room_for(int rows) { return (float)(33 - __builtin_clz(rows | 1)); }  // log2, up, and one
 struct Running {
-  float top, ref, sum;  // ref: top, or 0 where that is -inf
+  float top, ref, sum;  // the reference; ref: top, or 0 where that is -inf
   float keep;           // what the sums of V so far have still to be multiplied by
   bool moved;           // whether that is not one for some lane of the wave
 };
 __device__ __forceinline__ Running none_yet() { return Running{-INFINITY, 0.0f, 0.0f, 1.0f, false}; }
 // ... by the maximum of this half's rows (of the products, not yet scaled). A branch that stays one: without the statement in it
-// both sides are computed.
-__device__ __forceinline__ void take_maximum(float mx, float scale2, Running &run) {
+// both sides are computed. above: how far the reference lies above the maximum then, and slack: how far it may lie below.
+__device__ __forceinline__ void take_maximum(float mx, float scale2, Running &run, float slack = kSlack, float above = 0.0f) {
   mx = over_halves(mx, [](float x, float y) { return fmaxf(x, y); }) * scale2;
-  if (__any(mx > run.top + kSlack)) {
+  if (__any(mx > run.top + slack)) {
     asm volatile("" ::: "memory");
-    const float now = mx > run.top + kSlack ? mx : run.top;
+    const float now = mx > run.top + slack ? mx + above : run.top;
     run.ref = now == -INFINITY ? 0.0f : now;
     run.keep = now == run.top ? 1.0f : __builtin_amdgcn_exp2f(run.top - run.ref);
     run.sum *= run.keep;
@@ -252,13 +262,14 @@ __device__ __forceinline__ void take_maximum(float mx, float scale2, Running &ru
     run.moved = true;
   }
 }
-// Logits of a block to weights. CAREFUL with a mode other than kFinite: the weights become ones.
+// Logits of a block to weights. CAREFUL: with a reference `room` above the maximum, and with a mode other than kFinite the weights become ones.
 template <bool CAREFUL>
-__device__ __forceinline__ void to_weights(f32x16_p &z, float scale2, Running &run, int mode) {
+__device__ __forceinline__ void to_weights(f32x16_p &z, float scale2, Running &run, int mode, float room = 0.0f) {
   float mx = z[0];
 #pragma unroll
   for (int r = 1; r < 16; ++r) mx = fmaxf(mx, z[r]);
-  take_maximum(mx, scale2, run);
+  if (CAREFUL) take_maximum(mx, scale2, run, -room, room);
+  else take_maximum(mx, scale2, run);
   float part[4];  // the block's own sum first: a long list has thousands of blocks
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
@@ -307,7 +318,8 @@ __device__ __forceinline__ void take_marks(Marks &marks, f32x16_p (&acc)[DTILES]
     }
 }
 
-// Partial sums joined: what is infinite or NaN weighs in, however little its part weighs.
+// Partial results joined with weights that add up to one, so that nothing in between is larger than the largest part: what is infinite or NaN
+// weighs in, however little its part weighs.
 __device__ __forceinline__ f32x4_p add_part(f32x4_p num, const f32x4_p &x, float f) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) num[e] = fabsf(x[e]) < INFINITY ? fmaf(x[e], f, num[e]) : num[e] + x[e];

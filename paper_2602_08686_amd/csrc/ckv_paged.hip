@@ -16,7 +16,7 @@
 //
 // What a token does not see must not touch its result even if it is infinite or NaN, and zero times infinity is NaN: where a sweep leaves
 // something that is not finite, the workgroup sweeps again, with V's finite components only, and twice more for where its
-// infinite and NaN ones are.
+// infinite and NaN ones are. Sums that are beyond fp32 where their mean is not get a reference there that leaves them room.
 #include "ckv_paged.h"
 
 namespace ckv {
@@ -249,6 +249,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
   __syncthreads();
   if (s_undefined) {  // the same for all waves, as there are barriers in the sweeps; one block after the other
     Marks marks;
+    const float room = room_for(range.end);
 #pragma unroll 1
     for (int mode = kUp; mode <= kFinite; ++mode) {
       begin();
@@ -268,7 +269,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
           f32x16_p z;
           first_product<DT, DH>(s_k[(stage - first) & 1] + k * HALF, lane, qf, z);
           hide(z, stage * kStageRows + 32 * k);
-          to_weights<true>(z, a.scale2, run, mode);
+          to_weights<true>(z, a.scale2, run, mode, room);
           if (mode == kFinite) rescale(acc, run);  // marks are counted, whatever the row behind them weighs
           second_product<DT, DH, true>(s_v[(stage - first) & 1] + k * HALF, lane, as_operand<DT>(z), acc, mode);
         }
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
       const f32x4_p x = {acc[t][4 * r], acc[t][4 * r + 1], acc[t][4 * r + 2], acc[t][4 * r + 3]};
       const int d = 32 * t + block_row(4 * r, half);
       if (single) store_out<DT>(to, d, x * inv);
-      else *reinterpret_cast<f32x4_p *>(a.part + row * DH + d) = x;
+      else *reinterpret_cast<f32x4_p *>(a.part + row * DH + d) = x * inv;
     }
   if (half == 0) {
     if (single) store_lse(a, b, c, run.top, run.sum);
@@ -325,11 +326,14 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a)
   float sum = 0.0f, weight[SHARE];
 #pragma unroll
   for (int k = 0; k < SHARE; ++k) {
-    weight[k] = __builtin_amdgcn_exp2f(st[k].x - ref);
-    sum = fmaf(st[k].y, weight[k], sum);
+    weight[k] = st[k].y * __builtin_amdgcn_exp2f(st[k].x - ref);
+    sum += weight[k];
   }
 #pragma unroll
   for (int o = 1; o < PIECES; o <<= 1) sum += __shfl_xor(sum, o);
+  const float inv = inverse_sum(sum);
+#pragma unroll
+  for (int k = 0; k < SHARE; ++k) weight[k] *= inv;
   f32x4_p num = {0.0f, 0.0f, 0.0f, 0.0f};
   constexpr int BATCH = 8;
 #pragma unroll
@@ -348,7 +352,7 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a)
   }
   if (!valid) return;
   const Column c = column(a, unit, tile, local);
-  store_out<DT>(out_row(a, b, c), 4 * piece, num * inverse_sum(sum));
+  store_out<DT>(out_row(a, b, c), 4 * piece, num);
   if (piece == 0) store_lse(a, b, c, top, sum);
 }
 

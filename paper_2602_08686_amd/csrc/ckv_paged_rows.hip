@@ -31,7 +31,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
   __shared__ Offsets s_at[WAVES][32];
   __shared__ float2 s_stats[WAVES][32];
   __shared__ int s_last;
-  static_assert(32 * kMostChunks * sizeof(float2) <= sizeof(s_rows), "the chunks' sums are joined there too");
+  static_assert(kMostJoinedCols * kMostChunks * sizeof(float) <= sizeof(s_rows), "the chunks' weights lie there too");
   static_assert(32 * DH * 4 <= 2 * BLOCK, "a wave's sums take its rows' place");
 
   // a list's column tiles, which read the same rows, one behind the other
@@ -92,6 +92,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
 
   Running run;
   f32x16_p acc[I::DTILES];
+  const float room = room_for(range.end);
   auto sweep = [&](auto careful, int mode) CKV_INLINE {
     constexpr bool CAREFUL = decltype(careful)::value;
     run = none_yet();
@@ -131,7 +132,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
           if (block * 32 + row >= c.limit || (missing >> row & 1)) z[r] = -INFINITY;
         }
       }
-      to_weights<CAREFUL>(z, a.scale2, run, mode);
+      to_weights<CAREFUL>(z, a.scale2, run, mode, room);
       if (!CAREFUL || mode == kFinite) rescale(acc, run);  // marks are counted, whatever the rows behind them weigh
       if (more) wait_vm_at_most<LOADS + 1>();  // V; the next page numbers and K may be on their way
       else wait_vm_at_most<0>();
@@ -170,17 +171,21 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_stats[w][local].x);
     const float ref = top == -INFINITY ? 0.0f : top;
-    f32x4_p num = {0.0f, 0.0f, 0.0f, 0.0f};
+    float f[WAVES];
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
       const float2 st = s_stats[w][local];
-      const float f = __builtin_amdgcn_exp2f(st.x - ref);
-      sum = fmaf(st.y, f, sum);
-      num = add_part(num, *reinterpret_cast<const f32x4_p *>(s_rows[w] + local * DH * 4 + ((piece ^ local) % PIECES) * 16), f);
+      f[w] = __builtin_amdgcn_exp2f(st.x - ref);
+      sum = fmaf(st.y, f[w], sum);
     }
+    const float inv = inverse_sum(sum);
+    f32x4_p num = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w)
+      num = add_part(num, *reinterpret_cast<const f32x4_p *>(s_rows[w] + local * DH * 4 + ((piece ^ local) % PIECES) * 16), f[w] * inv);
     if (alone) {
       const Column o = column(a, unit, tile, local);
-      store_out<DT>(out_row(a, b, o), 4 * piece, num * inverse_sum(sum));
+      store_out<DT>(out_row(a, b, o), 4 * piece, num);
       if (piece == 0) store_lse(a, b, o, top, sum);
     } else {
       uint64_t *to = reinterpret_cast<uint64_t *>(a.part + (row0 + local) * DH + 4 * piece);
@@ -204,18 +209,20 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
   __syncthreads();
   if (!s_last) return;
   const size_t tile0 = row0 - (size_t)chunk * kRowsCols;
-  float2 *stats = reinterpret_cast<float2 *>(s_rows);  // [column][chunk]
-  for (int i = threadIdx.x; i < range.cols * used; i += WAVES * kWave) {
-    const int local = i / used, c = i % used;
-    stats[i] = __builtin_bit_cast(float2, load_across(reinterpret_cast<const uint64_t *>(a.stats + tile0 + (size_t)c * kRowsCols + local)));
+  float *weights = reinterpret_cast<float *>(s_rows);  // [column][chunk], a wave for a column, a lane for a chunk
+  for (int local = wave; local < range.cols; local += WAVES) {
+    float2 st = make_float2(-INFINITY, 0.0f);
+    if (lane < used)
+      st = __builtin_bit_cast(float2, load_across(reinterpret_cast<const uint64_t *>(a.stats + tile0 + (size_t)lane * kRowsCols + local)));
+    const float top = over_wave(st.x, -INFINITY, [](float x, float y) { return fmaxf(x, y); });
+    const float weight = st.y * __builtin_amdgcn_exp2f(st.x - (top == -INFINITY ? 0.0f : top));
+    const float sum = over_wave(weight, 0.0f, [](float x, float y) { return x + y; });
+    if (lane < used) weights[local * kMostChunks + lane] = weight * inverse_sum(sum);
+    if (lane == 0) store_lse(a, b, column(a, unit, tile, local), top, sum);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < range.cols * PIECES; i += WAVES * kWave) {
     const int local = i / PIECES, piece = i % PIECES;
-    const float2 *st = stats + local * used;
-    float top = st[0].x, sum = 0.0f;
-    for (int c = 1; c < used; ++c) top = fmaxf(top, st[c].x);
-    const float ref = top == -INFINITY ? 0.0f : top;
     const uint64_t *from = reinterpret_cast<const uint64_t *>(a.part + (tile0 + local) * DH + 4 * piece);
     f32x4_p num = {0.0f, 0.0f, 0.0f, 0.0f};
     constexpr int BATCH = 8;
@@ -226,16 +233,10 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
 #pragma unroll
         for (int e = 0; e < 2; ++e) x[j][e] = __builtin_bit_cast(float2, load_across(from + (size_t)min(c0 + j, used - 1) * (kRowsCols * DH / 2) + e));
 #pragma unroll
-      for (int j = 0; j < BATCH; ++j) {
-        if (c0 + j >= used) continue;
-        const float f = __builtin_amdgcn_exp2f(st[c0 + j].x - ref);
-        sum = fmaf(st[c0 + j].y, f, sum);
-        num = add_part(num, f32x4_p{x[j][0].x, x[j][0].y, x[j][1].x, x[j][1].y}, f);
-      }
+      for (int j = 0; j < BATCH; ++j)
+        if (c0 + j < used) num = add_part(num, f32x4_p{x[j][0].x, x[j][0].y, x[j][1].x, x[j][1].y}, weights[local * kMostChunks + c0 + j]);
     }
-    const Column o = column(a, unit, tile, local);
-    store_out<DT>(out_row(a, b, o), 4 * piece, num * inverse_sum(sum));
-    if (piece == 0) store_lse(a, b, o, top, sum);
+    store_out<DT>(out_row(a, b, column(a, unit, tile, local)), 4 * piece, num);
   }
   if (wave == 0 && lane < used) store_across(marks + lane, (tag_t)0);  // a replay of this launch has the same tag
 }

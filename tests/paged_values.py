@@ -56,3 +56,15 @@ BAD = {d: value for value, d in LOST.items()}
 def earlier(c, near, far, logit):
     """Row `near` of V is not finite and row `far` outweighs it by `logit`; component 9 has infinities of both signs, in rows of their own."""
     return make(c, {near: (None, dict(BAD)), near + 1: (None, {9: INF}), near + 2: (None, {9: -INF}), far: (logit, {})})
+
+
+def high(c, rise, value, sign, infinite):
+    """All of V at +-value, near the type's largest: every weighted mean is finite, the sums of weights times V are not. rise: logits grow with the
+    row, so that the softmax's reference keeps moving. infinite: one row holds an infinity and a NaN beside it."""
+    rng = np.random.default_rng(1)
+    rows = int(c["lengths"].max())
+    v = {r: {0: value if sign == "same" or rng.random() < 0.7 else -value, **({} if not (infinite and r == 7) else {3: INF, 5: NAN})} for r in range(rows)}
+    return make(c, {r: (rise * r, x) for r, x in v.items()}, v_all=value)
+
+
+HIGH = [(0.0, 1e37, "same", False), (0.02, 3e38, "same", False), (0.25, 3e38, "mixed", False), (-0.02, 2e38, "mixed", True)]

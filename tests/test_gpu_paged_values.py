@@ -21,3 +21,9 @@ def test_what_is_seen_and_not_finite_stays(c, near, far, logit):
     if far >= int(c["lengths"].min()) - c["n"]:
         far = 100
     _run(c, pv.earlier(c, near, far, logit))
+
+
+@pytest.mark.parametrize("rise,value,sign,infinite", pv.HIGH)
+@pytest.mark.parametrize("c", pv.FEW + pv.MANY, ids=range(len(pv.FEW + pv.MANY)))
+def test_a_mean_of_large_values_is_finite(c, rise, value, sign, infinite):
+    _run(c, pv.high(c, rise, value, sign, infinite))

@@ -22,3 +22,9 @@ def test_what_is_seen_and_not_finite_stays(lib_path, c, near, far):  # noqa: F81
     if far >= int(c["lengths"].min()) - c["n"]:
         far = 100
     in_child(_run, lib_path, c, pv.earlier, near, far, 300.0)
+
+
+@pytest.mark.parametrize("rise,value,sign,infinite", pv.HIGH)
+@pytest.mark.parametrize("c", pv.FEW + pv.MANY, ids=range(len(pv.FEW + pv.MANY)))
+def test_a_mean_of_large_values_is_finite(lib_path, c, rise, value, sign, infinite):  # noqa: F811
+    in_child(_run, lib_path, c, pv.high, rise, value, sign, infinite)
