@@ -1,4 +1,5 @@
-"""ctypes binding of libckv.so: the same calls as ``include/ckv.h``, argument marshalling only.
+"""ctypes binding of libckv.so: the same calls as ``include/ckv.h``, argument marshalling only; the calls on paged caches also hold their tensors
+against what params, pages and rotation describe (``csrc/ckv_tensors.cpp``).
 
 PyTorch supplies device memory and the current HIP stream; every step of the retention path runs in
 the library's kernels. There is no fallback: if the library is missing, loading raises.
@@ -13,6 +14,7 @@ import torch
 
 _LIB_PATH = Path(__file__).resolve().parent / "libckv.so"
 _lib = None
+_tensors = None
 
 CKV_OK, CKV_EINVAL, CKV_EUNSUPPORTED, CKV_EWORKSPACE, CKV_EHIP = range(5)
 CKV_F32, CKV_BF16 = 0, 1
@@ -124,6 +126,19 @@ def load(path: Optional[Path] = None):
     return lib
 
 
+def load_tensors():
+    """The checks of the paged caches' tensors (once). Raises if they have not been built."""
+    global _tensors
+    if _tensors is None:
+        try:
+            from . import _tensors as built
+        except ImportError as e:
+            raise FileNotFoundError("_tensors.so is missing or built for another PyTorch: build it with "
+                                    "`python -m paper_2602_08686_amd.build`. There is no fallback path.") from e
+        _tensors = built
+    return _tensors
+
+
 def status_string(status: int) -> str:
     return load().ckv_status_string(int(status)).decode()
 
@@ -180,6 +195,16 @@ def _stream(stream) -> ctypes.c_void_p:
     if not torch.cuda.is_initialized():
         return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)  # initialises, or says why it cannot
     return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+
+
+def _place(stream):
+    """(GPU, handle) of the given stream, or of the current one of the current device; (-1, None) as long as no tensor can be on one."""
+    if stream is not None:
+        return stream.device_index, stream.cuda_stream
+    if not torch.cuda.is_initialized():
+        return -1, None
+    device = torch._C._cuda_getDevice()
+    return device, torch._C._cuda_getCurrentRawStream(device)
 
 
 def _check(status: int, where: str):
@@ -341,18 +366,20 @@ def pages_for(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor)
 
 
 def ckv_norm_rotate(params, rotation, q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out, count=None, stream=None):
-    _check(load().ckv_norm_rotate(ctypes.byref(params), ctypes.byref(rotation), _at(q), _at(k), _at(positions), _at(inv_freq),
-                                  _at(q_weight), _at(k_weight), _at(count), _at(q_out), _at(k_out), _stream(stream)),
-           "ckv_norm_rotate")
+    """Raises a ValueError for a tensor that is not as params, rotation and the header describe it, as the calls below do."""
+    device, stream = _place(stream)
+    at = load_tensors().norm_rotate(params, rotation, device, q, k, positions, inv_freq, q_weight, k_weight, count, q_out, k_out)
+    _check(load().ckv_norm_rotate(ctypes.byref(params), ctypes.byref(rotation), *at, stream), "ckv_norm_rotate")
 
 
 def ckv_paged_append(params, rotation, pages, k, v, k_pages, v_pages, table, length, count=None, positions=None, inv_freq=None,
                      k_weight=None, q=None, q_weight=None, q_out=None, stream=None):
     """rotation may be None: plain copies (rows that the retention step kept)."""
-    _check(load().ckv_paged_append(ctypes.byref(params), None if rotation is None else ctypes.byref(rotation), ctypes.byref(pages),
-                                   _at(q), _at(k), _at(v), _at(positions), _at(inv_freq), _at(q_weight), _at(k_weight),
-                                   _at(table), _at(length), _at(count), _at(k_pages), _at(v_pages), _at(q_out),
-                                   _stream(stream)), "ckv_paged_append")
+    device, stream = _place(stream)
+    at = load_tensors().paged_append(params, rotation, pages, device, q, k, v, positions, inv_freq, q_weight, k_weight, table, length,
+                                     count, k_pages, v_pages, q_out)
+    _check(load().ckv_paged_append(ctypes.byref(params), None if rotation is None else ctypes.byref(rotation), ctypes.byref(pages), *at,
+                                   stream), "ckv_paged_append")
 
 
 def ckv_paged_workspace_bytes(params, n_rows) -> int:
@@ -367,10 +394,11 @@ def ckv_paged_attention(params, pages, q, k_pages, v_pages, table, length, n_row
         if out.dim() != 4 or out.stride(3) != 1:
             raise ValueError("out has to be [Bz,Hq,n,d] with a contiguous last axis")
         strides = (ctypes.c_int64 * 3)(*_row_strides(out, out.shape[3]))
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(load().ckv_paged_attention(ctypes.byref(params), ctypes.byref(pages), _at(q), _at(k_pages), _at(v_pages), _at(table),
-                                      _at(length), _at(count), int(n_rows), _at(out), strides, _at(lse), _at(workspace), nbytes,
-                                      _stream(stream)), "ckv_paged_attention")
+    device, stream = _place(stream)
+    *inputs, to, lse_at, ws_at, nbytes = load_tensors().paged_attention(params, pages, device, q, k_pages, v_pages, table, length, count, out, lse,
+                                                                        workspace)
+    _check(load().ckv_paged_attention(ctypes.byref(params), ctypes.byref(pages), *inputs, int(n_rows), to, strides, lse_at, ws_at, nbytes,
+                                      stream), "ckv_paged_attention")
 
 
 class LayerBuffers:

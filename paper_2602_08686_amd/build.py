@@ -1,15 +1,17 @@
-"""Builds libckv.so (the HIP kernels and their C ABI) for gfx950 with hipcc, in-tree."""
+"""Builds libckv.so (the HIP kernels and their C ABI) for gfx950 with hipcc, and the binding's part in C++ with g++, in-tree."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 INCLUDE = PKG.parent / "include"
 LIB = PKG / "libckv.so"
+TENSORS_LIB = PKG / "_tensors.so"
 HOOKS = PKG.parent / "tests" / "hooks"
 HOOKS_LIB = HOOKS / "libckv_hooks.so"
 SCAN_SOURCES = ["ckv_scan_bf16_d128_nq78.hip", "ckv_scan_bf16_d128_nq56.hip", "ckv_scan_bf16_d64_nq78.hip",
@@ -59,6 +61,20 @@ def build_library(verbose: bool = False) -> Path:
     return LIB
 
 
+def build_tensors() -> Path:
+    """Compile what checks the tensors of the paged cache's calls (host code only: a Python module on PyTorch's C++ types)."""
+    import torch
+    from torch.utils import cpp_extension
+
+    includes = [f"-I{p}" for p in (*cpp_extension.include_paths(), sysconfig.get_paths()["include"], INCLUDE)]
+    tmp = TENSORS_LIB.with_suffix(f".tmp{os.getpid()}.so")
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *includes, str(CSRC / "ckv_tensors.cpp"),
+                    f"-L{Path(torch.__file__).parent / 'lib'}", "-ltorch_python", "-ltorch", "-lc10", "-o", str(tmp)], check=True)
+    os.replace(tmp, TENSORS_LIB)
+    return TENSORS_LIB
+
+
 def build_probes() -> list:
     """Compile the measurement probes under probes/ (stand-alone HIP programs; not part of the library)."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -88,4 +104,4 @@ if __name__ == "__main__":
     if len(sys.argv) > 1 and sys.argv[1] == "probes":
         print(*build_probes(), sep="\n")
     else:
-        print(build_library(verbose=True))
+        print(build_library(verbose=True), build_tensors(), sep="\n")
