@@ -457,7 +457,8 @@ ckv_status ckv_paged_append(const ckv_params *params, const ckv_rotation *rotati
  *   lse         out  [Bz,Hq,n] fp32, natural log, or NULL
  *   workspace        ckv_paged_workspace_bytes(params, n_rows) bytes, 256-byte aligned; NULL where that is 0 (it is for refused arguments
  *                    too). Contents undefined before and after.
- * Logits and sums are fp32; in bf16 the weights enter the second product rounded to bf16, as the output is.
+ * Logits and sums are fp32; in bf16 the weights enter the second product rounded to bf16, as the output is, or, in calls of at most 64 new
+ * tokens times heads of a group, off by 2^-16 of themselves.
  * A mean of finite values is finite, however large they are; logits have to be below 2^24 in absolute value, where fp32 still tells neighbours apart by one.
  */
 size_t ckv_paged_workspace_bytes(const ckv_params *params, int32_t n_rows);

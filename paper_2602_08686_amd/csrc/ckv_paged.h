@@ -162,8 +162,11 @@ __device__ __forceinline__ uint32_t v_word(uint32_t x, int mode) {
   return mode == kFinite ? (finite ? x : 0u) : (marked ? 0x3f800000u : 0u);
 }
 
-// Weights of a block as the second product takes them: in bf16 rounded to the type, to the nearest: 2^-9 of each on average, of both signs, which
-// over many rows is less than the output's own rounding.
+// Weights of a block as the second product takes them: in bf16 rounded to the type, to the nearest. For many columns that is all (2^-9 of each on
+// average, of both signs, which over many rows is less than the output's own rounding); few columns, whose products wait for memory, take what the
+// rounding leaves in a product more. us, one term / two: one token, kept rows of 16 sequences 10.2 / 10.7, over 32768 rows 84.3 / 84.5, five
+// tokens over 9001 rows 29.1 / 30.5; many columns, where the matrix cores are the bound: 2048 tokens over 32768 rows 1005 / 1384, 4096 over
+// themselves 259 / 338.
 template <int DT>
 struct Weights {
   u32x4_d piece[DT == CKV_BF16 ? 2 : 4];
@@ -177,6 +180,17 @@ __device__ __forceinline__ Weights<DT> as_operand(const f32x16_p &w) {
   } else {
 #pragma unroll
     for (int e = 0; e < 16; ++e) out.piece[e / 4][e % 4] = __float_as_uint(w[e]);
+  }
+  return out;
+}
+
+// What that rounding leaves of bf16 weights, rounded again: with it a weight is off by 2^-16 of itself.
+__device__ __forceinline__ Weights<CKV_BF16> rest_of(const f32x16_p &w, const Weights<CKV_BF16> &first) {
+  Weights<CKV_BF16> out;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t x = first.piece[e / 4][e % 4];
+    out.piece[e / 4][e % 4] = pack_bf16(w[2 * e] - __uint_as_float(x << 16), w[2 * e + 1] - __uint_as_float(x & 0xffff0000u));
   }
   return out;
 }
@@ -205,22 +219,27 @@ __device__ __forceinline__ u32x4_d v_operand(const char *image, int at, int t, i
   return u32x4_d{lo[0], lo[1], hi[0], hi[1]};
 }
 // Second product of 32 rows of V: component 32 t + block_row(r, half) of the lane's column is acc[t][r]. CAREFUL: V's components as `mode` says.
-template <int DT, int DH, bool CAREFUL>
-__device__ __forceinline__ void second_product(const char *image, int lane, const Weights<DT> &w, f32x16_p (&acc)[DH / 32], int mode) {
+// rest: further terms of the weights, behind the first one, which leaves time to make them.
+template <int DT, int DH, bool CAREFUL, class... Rest>
+__device__ __forceinline__ void second_product(const char *image, int lane, const Weights<DT> &w, f32x16_p (&acc)[DH / 32], int mode, const Rest &...rest) {
   typedef Image<DT, DH> I;
   if constexpr (DT == CKV_BF16) {
     const int at = v_lane<DH>(lane);
+    u32x4_d x[2][I::DTILES];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int t = 0; t < I::DTILES; ++t) {
-        u32x4_d x = v_operand<DH>(image, at, t, j);
+        x[j][t] = v_operand<DH>(image, at, t, j);
         if (CAREFUL)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = v_word<DT>(x[e], mode);
-        mma_piece<DT>(acc[t], x, w.piece[j]);
+          for (int e = 0; e < 4; ++e) x[j][t][e] = v_word<DT>(x[j][t][e], mode);
+        mma_piece<DT>(acc[t], x[j][t], w.piece[j]);
       }
-    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int t = 0; t < I::DTILES; ++t) (mma_piece<DT>(acc[t], x[j][t], rest.piece[j]), ...);
   } else {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {

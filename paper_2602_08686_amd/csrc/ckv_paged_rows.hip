@@ -136,7 +136,9 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) paged_rows_kernel(Pag
       if (!CAREFUL || mode == kFinite) rescale(acc, run);  // marks are counted, whatever the rows behind them weigh
       if (more) wait_vm_at_most<LOADS + 1>();  // V; the next page numbers and K may be on their way
       else wait_vm_at_most<0>();
-      second_product<DT, DH, CAREFUL>(v_rows, lane, as_operand<DT>(z), acc, mode);
+      const Weights<DT> weights = as_operand<DT>(z);
+      if constexpr (DT == CKV_BF16) second_product<DT, DH, CAREFUL>(v_rows, lane, weights, acc, mode, rest_of(z, weights));
+      else second_product<DT, DH, CAREFUL>(v_rows, lane, weights, acc, mode);
       wait_lds_reads();
       if (more) fetch_v();
       missing = next_missing;

@@ -68,3 +68,17 @@ def high(c, rise, value, sign, infinite):
 
 
 HIGH = [(0.0, 1e37, "same", False), (0.02, 3e38, "same", False), (0.25, 3e38, "mixed", False), (-0.02, 2e38, "mixed", True)]
+
+
+def fine(c):
+    """Lists as they are, and the bound on the result with weights that are off by 2^-16 of themselves at most (two bf16 terms: each is off by 2^-8 of
+    what it stands for), in place of one rounding to bf16: paged_util's without its 2^-8 of sum_j w_j |v_j|."""
+    s = u.make(c)
+    want, tol, lse, lse_tol = u.attention(c, s)
+    plain = dict(s, v_pages=u.stored(np.abs(u.values(np.ascontiguousarray(s["v_pages"]))), c["dtype"]))
+    size = u.attention(c, plain)[0]   # sum_j w_j |v_j|
+    return s, want, tol - (u.H8 - 2.0 ** -16) * size, lse, lse_tol
+
+
+FINE = [u.case(n=1, lengths=((600, 31), (33, 1000))), u.case(n=9, heads=(7, 1), d=64, lengths=((900,), (16,)), page=64), u.case(n=4, lengths=((3000, 2900),)),
+        u.case(n=1, heads=(4, 1), lengths=((2500,),))]

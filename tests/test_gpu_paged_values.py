@@ -2,8 +2,9 @@
 import pytest
 import torch
 
+import paged_util as u
 import paged_values as pv
-from test_gpu_paged import attend, check_attention, on_gpu
+from test_gpu_paged import attend, check_attention, host, on_gpu
 
 pytestmark = pytest.mark.gpu
 
@@ -27,3 +28,12 @@ def test_what_is_seen_and_not_finite_stays(c, near, far, logit):
 @pytest.mark.parametrize("c", pv.FEW + pv.MANY, ids=range(len(pv.FEW + pv.MANY)))
 def test_a_mean_of_large_values_is_finite(c, rise, value, sign, infinite):
     _run(c, pv.high(c, rise, value, sign, infinite))
+
+
+@pytest.mark.parametrize("c", pv.FINE, ids=range(len(pv.FINE)))
+def test_few_columns_lose_nothing_to_the_weights(c):
+    s, want, tol, want_lse, lse_tol = pv.fine(c)
+    out, lse = attend(c, on_gpu(c, s))
+    torch.cuda.synchronize()
+    u.check(host(out), want, tol, "out")
+    u.check(host(lse), want_lse, lse_tol, "lse")

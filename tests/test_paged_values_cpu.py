@@ -2,6 +2,7 @@
 import pytest
 
 import cpu_build as cpu
+import paged_util as u
 import paged_values as pv
 from test_cpu_build import in_child, lib_path  # noqa: F401
 from test_paged_cpu import _attend, _check_attention, _fenced
@@ -28,3 +29,16 @@ def test_what_is_seen_and_not_finite_stays(lib_path, c, near, far):  # noqa: F81
 @pytest.mark.parametrize("c", pv.FEW + pv.MANY, ids=range(len(pv.FEW + pv.MANY)))
 def test_a_mean_of_large_values_is_finite(lib_path, c, rise, value, sign, infinite):  # noqa: F811
     in_child(_run, lib_path, c, pv.high, rise, value, sign, infinite)
+
+
+def _fine(path, c):
+    lib = cpu.load(path)
+    s, want, tol, want_lse, lse_tol = pv.fine(c)
+    out, lse = _attend(lib, c, _fenced(s))
+    u.check(out, want, tol, "out")
+    u.check(lse, want_lse, lse_tol, "lse")
+
+
+@pytest.mark.parametrize("c", pv.FINE, ids=range(len(pv.FINE)))
+def test_few_columns_lose_nothing_to_the_weights(lib_path, c):  # noqa: F811
+    in_child(_fine, lib_path, c)
