@@ -37,6 +37,7 @@ def load(path):
     lib = ctypes.CDLL(path, mode=os.RTLD_LAZY)
     lib.ckv_workspace_bytes.restype = lib.ckv_decode_workspace_bytes.restype = lib.ckv_paged_workspace_bytes.restype = ctypes.c_size_t
     lib.emu_set_hook.argtypes = [HOOK]
+    lib.emu_launched.restype = ctypes.c_char_p
     return lib
 
 

@@ -7,6 +7,7 @@
 #include <sys/mman.h>
 #include <ucontext.h>
 
+#include <string>
 #include <vector>
 
 namespace emu {
@@ -36,6 +37,8 @@ ucontext_t scheduler;
 int current = -1;
 const std::function<void()> *work = nullptr;
 void (*hook)(int block, int barrier) = nullptr;
+std::string launched;
+bool dry = false;
 
 void fiber_main() {
   (*work)();
@@ -220,7 +223,9 @@ void read_transposed(const void *four_words, void *out) {
   for (int k = 0; k < 4; ++k) memcpy(static_cast<char *>(out) + 2 * k, all + 64 * (first + 4 * k + i / 4) + 2 * (i % 4), 2);
 }
 
-void launch(dim3 grid, dim3 block, const std::function<void()> &body) {
+void launch(const char *kernel, const char *from, dim3 grid, dim3 block, const std::function<void()> &body) {
+  launched += std::string(kernel) + "|" + from + "|" + std::to_string(grid.x) + "|" + std::to_string(grid.y) + "\n";
+  if (dry) return;
   const int n = (int)block.x;
   if (!stacks) stacks = static_cast<char *>(mmap(nullptr, kStack * 1024, PROT_READ | PROT_WRITE, MAP_PRIVATE | MAP_ANONYMOUS, -1, 0));
   grid_dim = grid;
@@ -239,6 +244,15 @@ void launch(dim3 grid, dim3 block, const std::function<void()> &body) {
 
 // A call before a workgroup starts (barrier -1) and before each of its barriers lets go (nullptr: none), for tests that change memory meanwhile.
 extern "C" void emu_set_hook(void (*h)(int block, int barrier)) { emu::hook = h; }
+// A line for every launch since the last call: the kernel as it is written, the function that launches it with its template arguments, the grid.
+extern "C" const char *emu_launched() {
+  static std::string last;
+  last.swap(emu::launched);
+  emu::launched.clear();
+  return last.c_str();
+}
+// Launches are written down, but not run.
+extern "C" void emu_set_dry(int on) { emu::dry = on != 0; }
 // x with lane `lane` replaced by the wave-uniform v.
 extern "C" int emu_write_lane(int v, int lane, int x) __asm("llvm.amdgcn.writelane.i32");
 extern "C" int emu_write_lane(int v, int lane, int x) { return emu::lane() == lane ? v : x; }

@@ -43,7 +43,7 @@ template <class T> hipError_t hipGetSymbolAddress(void **p, T &symbol) { *p = &s
 
 namespace emu {
 extern dim3 thread_idx, block_idx, block_dim, grid_dim;
-void launch(dim3 grid, dim3 block, const std::function<void()> &body);
+void launch(const char *kernel, const char *from, dim3 grid, dim3 block, const std::function<void()> &body);
 void barrier();
 int lane();
 // Every live lane of the wave puts `bytes` (at most 64) down and gets the array of all 64 lanes' values (zeros for lanes
@@ -76,7 +76,7 @@ void read_transposed(const void *four_words, void *out);  // of 16 bits, among 1
 #define blockDim emu::block_dim
 #define gridDim emu::grid_dim
 #define __syncthreads() emu::barrier()
-#define hipLaunchKernelGGL(kernel, grid, block, lds, stream, ...) emu::launch(grid, block, [=] { kernel(__VA_ARGS__); })
+#define hipLaunchKernelGGL(kernel, grid, block, lds, stream, ...) emu::launch(#kernel, __PRETTY_FUNCTION__, grid, block, [=] { kernel(__VA_ARGS__); })
 
 template <class T> T min(T a, T b) { return b < a ? b : a; }
 template <class T> T max(T a, T b) { return a < b ? b : a; }
