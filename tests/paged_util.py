@@ -227,7 +227,7 @@ ROWS = [
     case(dtype="f32", heads=(2, 2), n=5, lengths=((5, 5),), page=2, pool_token_major=True),
     case(d=64, heads=(6, 3), n=33, lengths=((1000, 1000, 1000),), rot_dim=48, page=256),
     case(heads=(8, 2), n=4, lengths=((2, 9), (-3, 4)), counts=((4, 9), (4, -1)), rot_dim=128, page=4),  # rows before the list, odd counts
-    case(d=64, heads=(40, 40), n=2, lengths=((2,) * 40,), norm=True, rot_dim=64, pairing=N, page=2),     # more heads than a workgroup takes
+    case(d=64, heads=(40, 40), n=2, lengths=((2,) * 40,), norm=True, rot_dim=64, pairing=N, page=2),     # a workgroup for each head
     case(heads=(18, 2), n=3, lengths=((3, 3),), norm=True, rot_dim=64, page=8, token_major=False),       # more queries than are in flight together
 ]
 

@@ -7,6 +7,11 @@ import test_gpu_paged as t
 pytestmark = pytest.mark.gpu
 
 
+@pytest.mark.parametrize("c", more.ROWS, ids=range(len(more.ROWS)))
+def test_rows_are_transformed_and_find_their_pages(c):
+    t.test_rows_are_transformed_and_find_their_pages(c)
+
+
 @pytest.mark.parametrize("c", more.MANY, ids=range(len(more.MANY)))
 def test_attention_over_pages(c):
     t.test_attention_over_pages(c)
