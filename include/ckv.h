@@ -377,8 +377,8 @@ ckv_status ckv_discarded_mass(const ckv_params *params, int32_t n_q, const float
  *
  *   length  in  [Bz,Hkv] int32: rows of the list with the call's new rows, which are its last ones (what is below 0 counts as 0)
  *   count   in  [Bz,Hkv] int32 or NULL: new rows of the list, clamped to [0, n]; NULL: n. New row i is row length - count + i of
- *               the list; rows i >= count are neither read nor written, in any tensor of the call. Query head h has the count and length of its
- *               KV head h / G.
+ *               the list; rows i >= count are neither read nor written, in any tensor of the call (their positions may be read).
+ *               Query head h has the count and length of its KV head h / G.
  *   table   in  int32 page numbers at table_stride over (batch, KV head), max_pages in a row. A page number outside [0, n_pages),
  *               or a row outside [0, max_pages * page_rows): nothing is written there, and attention does not see the row.
  * A page may be in several lists (a shared prefix), or several times in one, as long as no call appends a row of it twice. Appending and
@@ -402,8 +402,8 @@ typedef enum { CKV_PAIR_HALVES = 0, CKV_PAIR_NEIGHBOURS = 1 } ckv_pairing;
  * then the first rot_dim components turn by the angles a_i = position * inv_freq[i], i < rot_dim / 2, in pairs
  *     (y_i, y_{i + rot_dim/2}) (CKV_PAIR_HALVES) or (y_{2i}, y_{2i+1}) (CKV_PAIR_NEIGHBOURS):
  *     (y, y') -> (y cos a - y' sin a, y' cos a + y sin a).
- * Sums and products are fp32 (mean square + norm_eps has to be a normal fp32 number), angles fp64 reduced to a turn; one rounding to the
- * type at the end. With norm = 0 and rot_dim = 0 rows are copied bit for bit.
+ * Sums and products are fp32 (the sum of the squares has to be finite there and mean square + norm_eps a normal number), angles fp64 reduced
+ * to a turn; one rounding to the type at the end. With norm = 0 and rot_dim = 0 rows are copied bit for bit.
  */
 typedef struct {
   int32_t rot_dim;   /* 0 .. head_dim, a multiple of 8                                              */
@@ -448,7 +448,7 @@ ckv_status ckv_paged_append(const ckv_params *params, const ckv_rotation *rotati
  * sequence sees the rows j <= length - count + i of its head's list that are below n_rows and whose page number is in the pool:
  *     z[j] = softmax_scale * <q[b,h,i,:], k row j>,  lse = log sum_j exp z[j],  out = sum_j exp(z[j] - lse) * v row j
  * What a token does not see has no influence, whatever it holds (infinities and NaN included). A token that sees no row gets zeros and
- * lse = -inf. With n = 1 this is a decoding step; lse of a prompt's last W tokens is the `lse` of
+ * lse = -inf. A row whose logit is -infinity counts as one that is not seen. With n = 1 this is a decoding step; lse of a prompt's last W tokens is the `lse` of
  * ckv_window_scores, lse of two caches is what ckv_discarded_mass takes.
  *   n_rows      no list is longer, 1 .. max_pages * page_rows and at most 2^24; a bound near the lengths lets the call share its work out well
  *   q           in   [Bz,Hq,n,d] via q_stride

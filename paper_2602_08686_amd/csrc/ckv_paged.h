@@ -360,15 +360,15 @@ __device__ __forceinline__ void store_lse(const PagedArgs &a, int b, const Colum
 }
 
 constexpr int kRowsCols = 32;  // columns of a tile of paged_rows_kernel
-// Up to here it takes a call's columns, in tiles that read the same rows at the same time. bf16: two tiles (35 columns, 9k rows: 41 us with
-// paged_tile_kernel, 37; from three tiles on that one reads less). f32, where the products of the matrix cores take longer than the rows: their
-// shares of the rows are what keeps the chip busy (200 columns, 1k rows 20.0 -> 13.1, 256, 2k 37 -> 34, 2048, 4k the other way round).
+// Up to here it takes a call's columns, in tiles that read the same rows at the same time. bf16: two tiles (35 columns, 9k rows: 31.3 us with
+// paged_tile_kernel, 30.5, 63 columns 33.2, 32.0; from three tiles on that one reads less). f32, where the products of the matrix cores take longer than the rows: their
+// shares of the rows are what keeps the chip busy (200 columns, 1k rows 17.4 -> 13.1, 256, 2k 40 -> 34, 2048, 4k the other way round).
 constexpr int kMostRowsCols = 64, kMostRowsColsF32 = 256;
 // Columns of a call, and their product with the chunks, up to which a tile's chunks are joined in the launch that makes them: above, leaving and
 // reading the sums past the caches takes one workgroup longer than a kernel of many behind this one takes with them. us, two launches / one: one
-// token, 32/8 heads, 2000 rows 12.9 / 11.7 (4 x 8), batch 4, 32768 rows 87.0 / 85.8, 65000 rows 50.7 / 49.9 (4 x 32), 28/4 heads, batch 8,
-// 9001 rows 27.8 / 26.9 (7 x 8); but with four tokens 30.2 / 31.1 (28 x 8), with five 35.4 / 35.8 (32 x 4), f32, 256 tokens, 2000 rows
-// 34.0 / 36.9 (32 x 4). (A counter instead of the marks: 65000 rows 93, its 32 workgroups one behind the other.)
+// token, 32/8 heads, 2000 rows 12.7 / 11.3 (4 x 8), batch 4, 32768 rows 86.0 / 84.5, 65000 rows 50.1 / 48.3 (4 x 32), 28/4 heads, batch 8,
+// 9001 rows 26.9 / 25.7 (7 x 8); but with four tokens 29.4 / 30.6 (28 x 8), with five 30.5 / 32.4 (32 x 4), f32, 256 tokens, 2000 rows
+// 33.9 / 38.8 (32 x 4). (A counter instead of the marks: 65000 rows 93, its 32 workgroups one behind the other.)
 constexpr int kMostJoinedCols = 16;
 constexpr int kMostJoined = 128;
 void launch_paged_rows(const PagedArgs &a, bool bf16, int d, hipStream_t stream);

@@ -2,15 +2,15 @@
 //
 // Columns: the queries of a (batch element, KV head), G * i + head, so that neighbours see nearly the same rows and a row is read once
 // for all heads of a group. A workgroup takes a tile of columns, 32 per wave, and sweeps the rows that the last of them sees, in stages
-// of 64 (bf16) or 32 (f32) rows that go from memory to LDS without registers between and are read by all of its waves.
+// of 64 rows that go from memory to LDS without registers between and are read by all of its waves.
 // Rows x queries (32 x 32 matrix tiles, 16 or 2 components at a time) leaves a lane with 16 logits of one column, whose running
 // maximum and sum stay in the lane but for one exchange with the other half of the wave, and which are the operand of the second product as
 // they lie: the contraction over rows may be permuted if both operands agree, so V's operand takes the rows in the order that the
 // logits have. V lies in LDS as it does in memory and is transposed on its way into registers.
 // LDS images are swizzled in units that one cycle reads (16 bytes of eight rows of K, 32 bytes of four rows of V).
-// Measured: bf16, 32/8 heads of 128, 2048 new tokens behind 30720 rows: 1.00 ms, 1064 TFLOP/s of the two products, where a plain 8192^3
-// product reaches 1241; batch 2, 32/32 heads, up to 4096 tokens over themselves: 270 us, 827 TFLOP/s. A stage of 64 rows takes a wave 3720 cycles, in
-// half of which the matrix cores work; without operands from LDS it is 6 % less, without the softmax's sums 3 %, so that what is left is
+// Measured: bf16, 32/8 heads of 128, 2048 new tokens behind 30720 rows: 1.00 to 1.07 ms by card, up to 1064 TFLOP/s of the two products, where a
+// plain 8192^3 product reaches 1241; batch 2, 32/32 heads, up to 4096 tokens over themselves: 270 to 290 us, up to 827 TFLOP/s. A stage of 64 rows
+// takes a wave 3720 cycles, in 55 % of which the matrix cores work; without operands from LDS it is 6 % less, without the softmax's sums 3 %, so that what is left is
 // the issue of what stands beside the products, at the 1.93 GHz that the card holds under this load. (No gain: loads
 // spread over a step's slots, operands three slots ahead, priorities of waves.) f32: the f32 products' rate, a sixteenth of bf16's.
 //
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(WAVES *kWave, WAVES == 4 && DT == CKV_F32 && D
 
   begin();
   if (first < last) {
-    for (int i = 0; i < 2; ++i) {  // the first two stages' rows, each by its wave; the page numbers have one place
+    for (int i = 0; i < 2; ++i) {  // the first two stages' rows, each by its wave, one behind the other
       fetch_ids(first + i);
       wait_vm_at_most<0>();
       find_rows(first + i);
@@ -365,10 +365,11 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a)
 // themselves 162 / 151, batch 4 of 1024 tokens 59 / 56, but 512 tokens over themselves 23 / 27.
 // Of the tiles in f32 with rows of 512 bytes one fits a CU: for long lists chunks for one, 300 tokens, 8/1 heads, batch 3, 2000 rows 99 / 88, 80 tokens,
 // 8/2 heads, 20000 rows 116 / 92, 512 tokens, 32/8 heads, 4096 rows 300 / 296; but 101 tokens, 8/1 heads, batch 8, 523 rows 35 / 44.
-// Least rows of a chunk, us with half / these / twice: few columns, bf16, one token, 32/8 heads, 2000 rows 11.2 / 11.6 / 13.1, batch 4
-// 13.6 / 13.6 / 14.3; f32, 4/4 heads of 64, batch 4, 1000 rows 12.0 / 11.3 / 13.5, 200 tokens, 1024 rows 13.9 / 13.4 / 14.9; tiles, bf16, 512 tokens over
-// themselves 24.1 / 19.5 / 19.5; f32, heads of 64, 101 tokens, 523 rows (64 / 128) 24.3 / 29.6. One chunk up to 1024 (bf16) or 256 (f32) rows of few columns: 500 rows 9.4, two chunks 10.4; batch 16,
-// 544 rows 11.2, two chunks 11.7; but batch 4 over 2000 rows 19.6 with one, 13.6 with the rule's.
+// Least rows of a chunk, us with half / these / twice: few columns, bf16, one token, 32/8 heads, 2000 rows 10.8 / 11.4 / 12.7, batch 4
+// 12.6 / 12.6 / 14.3; f32, 4/4 heads of 64, batch 4, 1000 rows 11.4 / 10.8 / 13.1, 200 tokens, 1024 rows 13.9 / 13.1 / 15.5; tiles, bf16, 512 tokens over
+// themselves 24.1 / 19.5 / 19.5; f32, heads of 64, 101 tokens, 523 rows (64 / 128) 24.3 / 29.6. One chunk up to 1024 (bf16) or 256 (f32) rows
+// of few columns: 500 rows 10.1, two chunks 11.0; batch 16, 544 rows 10.7, two chunks 11.6, 1000 rows 16.9, two 16.3; but batch 4 over 2000 rows
+// 23.7 with one, 12.6 with the rule's.
 PagedPlan plan_paged(const Shape &s, int n_rows) {
   PagedPlan p;
   const bool bf16 = s.esize == 2;

@@ -5,9 +5,9 @@
 // loads go straight to LDS. K's place is free once the first product has read it and V's once the second has, so the next
 // 32 rows' K is on its way during the softmax and the second product, their V during the next first product. Page numbers
 // come the same way, one block further ahead; a lane per row turns them into offsets.
-// Measured: bf16, 32/8 heads of 128, batch 4, 32768 rows, one token 85.8 us, 6.3 TB/s of K and V; 65000 rows, batch 1 49.8 us, 5.3. Short lists are
-// a chain of latencies: batch 16, up to 544 rows 10.9 us, of which 1.8 until the page numbers, 1.4 more until K, 3.7 for three blocks
-// a wave and 3.2 for joining the waves. (Four waves, and two or four times as many chunks, were slower.)
+// Measured: bf16, 32/8 heads of 128, batch 4, 32768 rows, one token 85.9 us, 6.3 TB/s of K and V; 65000 rows, batch 1 48.3 us, 5.5. Short lists are
+// a chain of latencies: batch 16, up to 544 rows 11.4 us, in cycles of a mean workgroup 4500 until the page numbers, 2900 more until K, 6400 for
+// the first wave's two or three blocks and 7300 for waiting for the other waves and joining them. (Four waves, and two or four times as many chunks, were slower.)
 // Waves are joined in LDS in wave order, chunks in chunk order: by paged_merge_kernel, or where their sums are few in this launch. Each workgroup
 // then leaves its sums, past its own caches, and behind them a mark, the launch's tag (another value for every launch, which undefined memory
 // does not hold), and looks at the marks of its tile. Who finds all of them, which the last one to mark does unless somebody else has before,

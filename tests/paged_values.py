@@ -82,3 +82,10 @@ def fine(c):
 
 FINE = [u.case(n=1, lengths=((600, 31), (33, 1000))), u.case(n=9, heads=(7, 1), d=64, lengths=((900,), (16,)), page=64), u.case(n=4, lengths=((3000, 2900),)),
         u.case(n=1, heads=(4, 1), lengths=((2500,),))]
+
+
+def no_logit(c, minus_infinity):
+    """Rows whose logit is -infinity, V infinite or NaN beside it; or the same rows so far below the others that they weigh nothing in 64 bits either, V
+    finite: the results are the same."""
+    rows = {4: {3: INF}, 40: {3: NAN, 5: -INF}, 41: {}}
+    return make(c, {r: (-INF, v) if minus_infinity else (-800.0, {}) for r, v in rows.items()})

@@ -37,3 +37,10 @@ def test_few_columns_lose_nothing_to_the_weights(c):
     torch.cuda.synchronize()
     u.check(host(out), want, tol, "out")
     u.check(host(lse), want_lse, lse_tol, "lse")
+
+
+@pytest.mark.parametrize("c", [pv.FEW[0], pv.FEW[3], pv.FEW[5], pv.MANY[0], pv.MANY[2]], ids=range(5))
+def test_a_row_with_a_logit_of_minus_infinity_is_not_seen(c):
+    out, lse = attend(c, on_gpu(c, pv.no_logit(c, True)))
+    torch.cuda.synchronize()
+    check_attention(c, pv.no_logit(c, False), out, lse)

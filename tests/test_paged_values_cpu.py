@@ -42,3 +42,13 @@ def _fine(path, c):
 @pytest.mark.parametrize("c", pv.FINE, ids=range(len(pv.FINE)))
 def test_few_columns_lose_nothing_to_the_weights(lib_path, c):  # noqa: F811
     in_child(_fine, lib_path, c)
+
+
+def _no_logit(path, c):
+    lib = cpu.load(path)
+    _check_attention(c, pv.no_logit(c, False), *_attend(lib, c, _fenced(pv.no_logit(c, True))))
+
+
+@pytest.mark.parametrize("c", [pv.FEW[0], pv.FEW[3], pv.FEW[5], pv.MANY[0], pv.MANY[2]], ids=range(5))
+def test_a_row_with_a_logit_of_minus_infinity_is_not_seen(lib_path, c):  # noqa: F811
+    in_child(_no_logit, lib_path, c)
