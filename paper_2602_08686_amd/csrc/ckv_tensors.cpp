@@ -1,7 +1,7 @@
 // What the binding hands to the paged cache's calls: tensors as the structs of the call describe them, or a ValueError, and their addresses. A kernel
 // reads what an address says; a tensor of another type, shape or layout would be read past its end or in another order. In C++ because the
 // checks then take no longer than asking each tensor for its address did (host time of a call of eight tensors, the library's part aside: 1.2 us
-without checks, 0.9 with these; asked one by one from Python, the same questions take some 3 us).
+// without checks, 0.9 with these; asked one by one from Python, the same questions take some 3 us).
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <initializer_list>
