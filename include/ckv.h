@@ -11,7 +11,9 @@
  * the paper's layer-shared mode (ckv_alpha_accumulate, ckv_risk_struct, ckv_shared_utility,
  * ckv_compact_kv_shared), the depth mapping of compiled tables (ckv_map_table_depth), a decode-side consumer of the compact cache (ckv_decode_attention,
  * ckv_discarded_mass), and the calls of a cache that goes on: norm and position rotation of new rows (ckv_norm_rotate), their way into pages
- * (ckv_paged_append) and attention of new tokens over the pages (ckv_paged_attention).
+ * (ckv_paged_append) and attention of new tokens over the pages (ckv_paged_attention); for trees of drafted tokens ckv_tree_sees and
+ * ckv_paged_tree_attention; rows and pages that move (ckv_paged_compact, ckv_pages_copy) and lists that share pages, get some and give them
+ * back (ckv_pages_fork, ckv_pages_reserve, ckv_pages_free).
  *
  * Notation (paper Sec. 3-4): T = prompt length (keys/values cached at the end of prefill, the
  * observation window included), W = |Omega| = observation window (the last W query positions),
@@ -466,6 +468,110 @@ ckv_status ckv_paged_attention(const ckv_params *params, const ckv_pages *pages,
                                const void *v_pages, const int32_t *table, const int32_t *length, const int32_t *count, int32_t n_rows,
                                void *out, const int64_t *out_stride, float *lse, void *workspace, size_t workspace_bytes,
                                void *hip_stream);
+
+/*
+ * Trees of drafted tokens. Several continuations of a sequence are verified together: its new tokens are the nodes of a tree (or of several, whose roots
+ * all follow the rows in front of them), a token behind its parent in the call's order. What a token sees of the new ones is a word of bits:
+ * bit t % 64 of sees[b][i][t / 64] says whether token i sees token t.
+ *
+ * ckv_tree_sees makes them of parents: token i sees itself and what its parent sees, and stands one position behind it.
+ *   batch, n    sizes, 1 <= n <= 4096
+ *   parent      in   [batch,n] int32; a value that is not one of 0 .. i - 1 makes token i a root
+ *   start       in   [batch] int32: a root's position; may be NULL with positions
+ *   sees        out  [batch,n,ceil(n/64)] 64-bit words
+ *   positions   out  [batch,n] int32, what ckv_norm_rotate and ckv_paged_append take, or NULL
+ *
+ * ckv_paged_tree_attention is ckv_paged_attention with these words in place of the causal order among the new tokens: token i < count sees the rows
+ * j < length - count, and row length - count + t for t <= i where its bit t is set. Words of any origin do (a token without bits sees the rows in
+ * front of the new ones alone, and one that sees no row gets zeros and lse = -inf); bits of tokens behind i are not looked at. n is 65536 at most.
+ *   sees        in   [Bz,n,ceil(n/64)] 64-bit words, one set for all heads
+ *   the others       as for ckv_paged_attention, the workspace too
+ */
+ckv_status ckv_tree_sees(int32_t batch, int32_t n, const int32_t *parent, const int32_t *start, uint64_t *sees, int32_t *positions,
+                         void *hip_stream);
+ckv_status ckv_paged_tree_attention(const ckv_params *params, const ckv_pages *pages, const void *q, const void *k_pages,
+                                    const void *v_pages, const int32_t *table, const int32_t *length, const int32_t *count, int32_t n_rows,
+                                    const uint64_t *sees, void *out, const int64_t *out_stride, float *lse, void *workspace,
+                                    size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Rows that stay, moved together inside their pages: of the last `count` rows of a list (all of them with count NULL) those named by idx become
+ * the first, the list ends behind them. With first = length - count and m = kept clamped to [0, count] and to cap, for r < m
+ *     row first + r <- row first + idx[b,g,r]  (bit copies of keys and values),  length_out[b,g] = first + m
+ * This drops rejected tokens of a tree (count: its tokens, idx: the accepted path), or does in the pages what ckv_compact_kv does beside them
+ * (idx and kept: idx and count of ckv_select_topk). Rows behind length_out keep what they held or got; ckv_pages_free gives back their pages.
+ *   Of ckv_params batch, n_kv_heads, head_dim and dtype are used; the other fields have to be valid.
+ *   table, length, count  as above, but count is clamped to [0, length]
+ *   idx         in   numbers below count, ascending, none twice, at element strides idx_stride over (batch, KV head) (0: one for all heads);
+ *                    idx_stride NULL: [Bz,Hkv,cap]. A number that is not below count, or a row that is on no page: nothing is written for it.
+ *                    In another order rows get some row's former or present contents, nothing else is touched
+ *   cap         entries of a list in idx, >= 1
+ *   kept        in   [Bz,Hkv] int32
+ *   k_pages, v_pages  in/out; pages that are written are in no other list, or other lists see the change (ckv_pages_reserve gives lists pages of
+ *                    their own)
+ *   length_out  out  [Bz,Hkv] int32, not `length` itself
+ */
+ckv_status ckv_paged_compact(const ckv_params *params, const ckv_pages *pages, const int32_t *table, const int32_t *length, const int32_t *count,
+                             const int32_t *idx, const int64_t *idx_stride, int32_t cap, const int32_t *kept, void *k_pages, void *v_pages,
+                             int32_t *length_out, void *hip_stream);
+
+/*
+ * Whole pages, keys and values of all KV heads, from copy[i][0] to copy[i][1], i < n. Pairs with a number outside [0, n_pages), or twice the same, are
+ * skipped (what ckv_pages_reserve leaves of its array). No page is written twice, or written and read, in one call.
+ *   Of ckv_params n_kv_heads, head_dim and dtype are used, of ckv_pages not the table's fields. k_stride[1] = 0: pages of one head.
+ *   copy        in   [n,2] int32
+ */
+ckv_status ckv_pages_copy(const ckv_params *params, const ckv_pages *pages, const int32_t *copy, int32_t n, void *k_pages, void *v_pages,
+                          void *hip_stream);
+
+/*
+ * Which lists have which pages. Once for all pools that the lists describe (the layers of a model), beside the calls on each of them. An entry of a
+ * list names a page, or none with a value outside [0, n_pages) (these calls write -1). refs[p] is how many entries name page p, and bit p % 32 of
+ * taken[p / 32] whether any does: with lists without pages, all zeros. Both have to agree with the lists of all tables that
+ * share them; then all results are the same in every run. They go from call to call in stream order.
+ *   refs   in/out  [n_pages] int32         taken  in/out  [ceil(n_pages/32)] 32-bit words
+ *   table          int32 entries at table_stride over (batch, KV head); table_stride[1] = 0: one list for the heads of a batch element
+ * Numbers of rows are [batch,n_kv_heads] int32, and where heads have a list in common, it is long enough for the longest of them.
+ */
+typedef struct {
+  int32_t batch;           /* >= 1                                                                  */
+  int32_t n_kv_heads;      /* >= 1                                                                  */
+  int32_t n_pages;         /* pages of the pools, >= 1                                              */
+  int32_t page_rows;       /* as in ckv_pages                                                       */
+  int32_t max_pages;       /* as in ckv_pages; batch * n_kv_heads * max_pages < 2^31                */
+  int32_t reserved;        /* 0                                                                     */
+  int64_t table_stride[2]; /* as in ckv_pages; no two lists overlap                                 */
+} ckv_lists;
+
+/*
+ * Lists that become copies of others and share their pages (several answers to a prompt, beams): table_out[b] = table[parent[b]], or no pages with a
+ * parent outside [0, batch). The pages of the former lists of table_out are released, those of the new ones counted; `table` stays as it is (its
+ * own pages are released by ckv_pages_free, keep = NULL). A shared page that a list is to write into gets a copy by ckv_pages_reserve.
+ *   table       in   int32, table_stride        table_out  in/out  int32, table_stride, not overlapping `table`
+ *   parent      in   [batch] int32
+ *   length      in   [batch,n_kv_heads] int32, or NULL with length_out
+ *   length_out  out  length[parent[b]], or 0 without one; not `length` itself
+ */
+ckv_status ckv_pages_fork(const ckv_lists *lists, const int32_t *table, const int32_t *parent, int32_t *table_out, int32_t *refs,
+                          uint32_t *taken, const int32_t *length, int32_t *length_out, void *hip_stream);
+
+/*
+ * Makes rows [first, end) of every list such as can be written: entries of that range without a page get one, and entries whose page others name too get
+ * one of their own, with a pair (former page, new page) in `copy` for ckv_pages_copy on each pool. Where all that share a page ask for it, the
+ * last of them keeps it. New pages are the lowest-numbered free ones, in the order of the entries (batch, KV head, entry), pairs are in that order too.
+ * All or nothing: where there are too few free pages or too few places for pairs, only copy (no pairs) and result are written.
+ *   first, end  in   [batch,n_kv_heads] int32; nothing to do where end <= first, or behind max_pages * page_rows
+ *   copy        out  [n_copy,2] int32, pairs and behind them -1; n_copy >= 0 (copy may be NULL with 0)
+ *   result      out  [2] int32: pages (or places for pairs, if that is more) that are missing, 0 if all is done; pairs
+ */
+ckv_status ckv_pages_reserve(const ckv_lists *lists, int32_t *table, const int32_t *first, const int32_t *end, int32_t *refs, uint32_t *taken,
+                             int32_t *copy, int32_t n_copy, int32_t *result, void *hip_stream);
+
+/*
+ * Pages behind the first keep[b,g] rows of every list leave it (all of them with keep NULL), and are free where no other entry names them.
+ *   keep        in   [batch,n_kv_heads] int32, or NULL
+ */
+ckv_status ckv_pages_free(const ckv_lists *lists, int32_t *table, const int32_t *keep, int32_t *refs, uint32_t *taken, void *hip_stream);
 
 /* Static text for a status code; never NULL. */
 const char *ckv_status_string(ckv_status status);

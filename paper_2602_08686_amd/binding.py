@@ -27,6 +27,7 @@ EXPORTS = ("ckv_workspace_bytes", "ckv_window_lse", "ckv_window_lse_static_bytes
            "ckv_compact_kv", "ckv_retention_layer", "ckv_alpha_accumulate", "ckv_risk_struct", "ckv_shared_utility", "ckv_compact_kv_shared",
            "ckv_decode_workspace_bytes", "ckv_decode_attention", "ckv_discarded_mass", "ckv_map_table_depth",
            "ckv_norm_rotate", "ckv_paged_append", "ckv_paged_workspace_bytes", "ckv_paged_attention",
+           "ckv_tree_sees", "ckv_paged_tree_attention", "ckv_paged_compact", "ckv_pages_copy", "ckv_pages_fork", "ckv_pages_reserve", "ckv_pages_free",
            "ckv_status_string")
 
 
@@ -46,6 +47,13 @@ class CkvPages(ctypes.Structure):
     _fields_ = [
         ("page_rows", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("reserved", ctypes.c_int32),
         ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3), ("table_stride", ctypes.c_int64 * 2),
+    ]
+
+
+class CkvLists(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32), ("reserved", ctypes.c_int32), ("table_stride", ctypes.c_int64 * 2),
     ]
 
 
@@ -117,6 +125,21 @@ def load(path: Optional[Path] = None):
     lib.ckv_paged_workspace_bytes.restype = ctypes.c_size_t
     lib.ckv_paged_attention.argtypes = [pp, gp, vp, vp, vp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.ckv_paged_attention.restype = ctypes.c_int
+    i32, lp = ctypes.c_int32, ctypes.POINTER(CkvLists)
+    lib.ckv_tree_sees.argtypes = [i32, i32, vp, vp, vp, vp, vp]
+    lib.ckv_tree_sees.restype = ctypes.c_int
+    lib.ckv_paged_tree_attention.argtypes = [pp, gp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.ckv_paged_tree_attention.restype = ctypes.c_int
+    lib.ckv_paged_compact.argtypes = [pp, gp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp]
+    lib.ckv_paged_compact.restype = ctypes.c_int
+    lib.ckv_pages_copy.argtypes = [pp, gp, vp, i32, vp, vp, vp]
+    lib.ckv_pages_copy.restype = ctypes.c_int
+    lib.ckv_pages_fork.argtypes = [lp] + [vp] * 8
+    lib.ckv_pages_fork.restype = ctypes.c_int
+    lib.ckv_pages_reserve.argtypes = [lp, vp, vp, vp, vp, vp, vp, i32, vp, vp]
+    lib.ckv_pages_reserve.restype = ctypes.c_int
+    lib.ckv_pages_free.argtypes = [lp] + [vp] * 5
+    lib.ckv_pages_free.restype = ctypes.c_int
     lib.ckv_map_table_depth.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, vp, ctypes.c_int32, vp]
     lib.ckv_map_table_depth.restype = ctypes.c_int
     lib.ckv_status_string.argtypes = [ctypes.c_int]
@@ -386,19 +409,115 @@ def ckv_paged_workspace_bytes(params, n_rows) -> int:
     return int(load().ckv_paged_workspace_bytes(ctypes.byref(params), int(n_rows)))
 
 
+def _out_strides(out):
+    """Strides of an output [Bz,Hq,n,d] as the library takes them; None: dense."""
+    if out.is_contiguous():
+        return None
+    if out.dim() != 4 or out.stride(3) != 1:
+        raise ValueError("out has to be [Bz,Hq,n,d] with a contiguous last axis")
+    return (ctypes.c_int64 * 3)(*_row_strides(out, out.shape[3]))
+
+
 def ckv_paged_attention(params, pages, q, k_pages, v_pages, table, length, n_rows, out, lse=None, workspace=None, count=None,
                         stream=None):
     """out [Bz,Hq,n,d], any strides over the first three axes."""
-    strides = None
-    if not out.is_contiguous():
-        if out.dim() != 4 or out.stride(3) != 1:
-            raise ValueError("out has to be [Bz,Hq,n,d] with a contiguous last axis")
-        strides = (ctypes.c_int64 * 3)(*_row_strides(out, out.shape[3]))
+    strides = _out_strides(out)
     device, stream = _place(stream)
     *inputs, to, lse_at, ws_at, nbytes = load_tensors().paged_attention(params, pages, device, q, k_pages, v_pages, table, length, count, out, lse,
                                                                         workspace)
     _check(load().ckv_paged_attention(ctypes.byref(params), ctypes.byref(pages), *inputs, int(n_rows), to, strides, lse_at, ws_at, nbytes,
                                       stream), "ckv_paged_attention")
+
+
+def ckv_tree_sees(parent, start, sees, positions=None, stream=None):
+    """parent [batch,n] int32; start [batch] int32; sees [batch,n,ceil(n/64)] int64, a bit for each token that is seen; positions [batch,n]
+    int32 or None (start then may be None, too)."""
+    if not isinstance(parent, torch.Tensor) or parent.dim() != 2:
+        raise ValueError("parent has to be int32 [batch,n] contiguous")
+    batch, n = parent.shape
+    device, stream = _place(stream)
+    at = load_tensors().tree_sees(device, batch, n, parent, start, sees, positions)
+    _check(load().ckv_tree_sees(batch, n, *at, stream), "ckv_tree_sees")
+
+
+def ckv_paged_tree_attention(params, pages, q, k_pages, v_pages, table, length, n_rows, sees, out, lse=None, workspace=None, count=None,
+                             stream=None):
+    """sees [Bz,n,ceil(n/64)] int64 (ckv_tree_sees); the others as for ckv_paged_attention."""
+    strides = _out_strides(out)
+    device, stream = _place(stream)
+    *inputs, sees_at, to, lse_at, ws_at, nbytes = load_tensors().paged_tree_attention(params, pages, device, q, k_pages, v_pages, table, length, count,
+                                                                                      sees, out, lse, workspace)
+    _check(load().ckv_paged_tree_attention(ctypes.byref(params), ctypes.byref(pages), *inputs, int(n_rows), sees_at, to, strides, lse_at, ws_at,
+                                           nbytes, stream), "ckv_paged_tree_attention")
+
+
+def pool_params(k_pages: torch.Tensor, table: torch.Tensor) -> CkvParams:
+    """ckv_params of a call on the pages alone: pools [n_pages,Hkv,page_rows,d], lists [Bz,...]."""
+    if k_pages.dim() != 4 or table.dim() not in (2, 3):
+        raise ValueError("k_pages has to be [n_pages,Hkv,page_rows,d], table [Bz,max_pages] or [Bz,Hkv,max_pages]")
+    return make_params(batch=table.shape[0], n_q_heads=k_pages.shape[1], n_kv_heads=k_pages.shape[1], head_dim=k_pages.shape[3], seq_len=1, window=1,
+                       dtype=k_pages.dtype, pool=POOL_NONE, pool_kernel=1, budget=1, cap=1)
+
+
+def ckv_paged_compact(params, pages, k_pages, v_pages, table, length, idx, kept, length_out, count=None, stream=None):
+    """idx [Bz,cap] (one for all heads) or [Bz,Hkv,cap] int32, any strides with a contiguous last axis; kept, length_out [Bz,Hkv] int32."""
+    if not isinstance(idx, torch.Tensor) or idx.dim() not in (2, 3):
+        raise ValueError("idx has to be int32 [Bz,cap] or [Bz,Hkv,cap] with a contiguous last axis")
+    strides = (ctypes.c_int64 * 2)(idx.stride(0), idx.stride(1) if idx.dim() == 3 else 0)
+    device, stream = _place(stream)
+    table_at, length_at, count_at, idx_at, *rest = load_tensors().paged_compact(params, pages, device, table, length, count, idx, kept, k_pages,
+                                                                                v_pages, length_out)
+    _check(load().ckv_paged_compact(ctypes.byref(params), ctypes.byref(pages), table_at, length_at, count_at, idx_at, strides, idx.shape[-1],
+                                    *rest, stream), "ckv_paged_compact")
+
+
+def ckv_pages_copy(params, pages, k_pages, v_pages, copy, stream=None):
+    """copy [n,2] int32: pairs (from, to)."""
+    if not isinstance(copy, torch.Tensor) or copy.dim() != 2:
+        raise ValueError("copy has to be int32 [n,2] contiguous")
+    device, stream = _place(stream)
+    copy_at, *pools = load_tensors().pages_copy(params, pages, device, copy.shape[0], copy, k_pages, v_pages)
+    if copy.shape[0]:
+        _check(load().ckv_pages_copy(ctypes.byref(params), ctypes.byref(pages), copy_at, copy.shape[0], *pools, stream), "ckv_pages_copy")
+
+
+def lists_for(table: torch.Tensor, *, n_kv_heads, n_pages, page_rows) -> CkvLists:
+    """ckv_lists of a table [Bz,max_pages] (one list for all heads of a sequence) or [Bz,Hkv,max_pages]."""
+    if table.dtype != torch.int32 or table.dim() not in (2, 3) or (table.shape[-1] > 1 and table.stride(-1) != 1):
+        raise ValueError("table has to be int32 [Bz,max_pages] or [Bz,Hkv,max_pages] with a contiguous last axis")
+    if table.dim() == 3 and table.shape[1] != n_kv_heads:
+        raise ValueError(f"table has to be [Bz,{n_kv_heads},max_pages]")
+    out = CkvLists(table.shape[0], int(n_kv_heads), int(n_pages), int(page_rows), table.shape[-1], 0)
+    out.table_stride[0] = table.stride(0) if table.shape[0] > 1 else table.shape[-1] * (n_kv_heads if table.dim() == 3 else 1)
+    out.table_stride[1] = 0 if table.dim() == 2 else table.stride(1) if n_kv_heads > 1 else table.shape[-1]
+    return out
+
+
+def page_counts(n_pages, device="cuda"):
+    """(refs, taken) of pools whose pages no list has."""
+    return torch.zeros(n_pages, dtype=torch.int32, device=device), torch.zeros((n_pages + 31) // 32, dtype=torch.int32, device=device)
+
+
+def ckv_pages_fork(lists, table, parent, table_out, refs, taken, length=None, length_out=None, stream=None):
+    """table and table_out as lists describe them; parent [Bz] int32; refs and taken as page_counts makes them, length and length_out [Bz,Hkv] int32."""
+    device, stream = _place(stream)
+    at = load_tensors().pages_fork(lists, device, table, parent, table_out, refs, taken, length, length_out)
+    _check(load().ckv_pages_fork(ctypes.byref(lists), *at, stream), "ckv_pages_fork")
+
+
+def ckv_pages_reserve(lists, table, first, end, refs, taken, copy, result, stream=None):
+    """first, end [Bz,Hkv] int32; copy [n,2] int32 or None; result [2] int32."""
+    n = 0 if copy is None else copy.shape[0]
+    device, stream = _place(stream)
+    *at, copy_at, result_at = load_tensors().pages_reserve(lists, device, n, table, first, end, refs, taken, copy, result)
+    _check(load().ckv_pages_reserve(ctypes.byref(lists), *at, copy_at, n, result_at, stream), "ckv_pages_reserve")
+
+
+def ckv_pages_free(lists, table, keep, refs, taken, stream=None):
+    """keep [Bz,Hkv] int32 rows, or None: all pages."""
+    device, stream = _place(stream)
+    at = load_tensors().pages_free(lists, device, table, keep, refs, taken)
+    _check(load().ckv_pages_free(ctypes.byref(lists), *at, stream), "ckv_pages_free")
 
 
 class LayerBuffers:

@@ -738,10 +738,9 @@ extern "C" size_t ckv_paged_workspace_bytes(const ckv_params *params, int32_t n_
   return plan.workgroups > kMostPagedWorkgroups ? 0 : align256(plan.workspace_bytes);
 }
 
-extern "C" ckv_status ckv_paged_attention(const ckv_params *params, const ckv_pages *pages, const void *q, const void *k_pages,
-                                          const void *v_pages, const int32_t *table, const int32_t *length, const int32_t *count,
-                                          int32_t n_rows, void *out, const int64_t *out_stride, float *lse, void *workspace,
-                                          size_t workspace_bytes, void *hip_stream) {
+static ckv_status attend(const ckv_params *params, const ckv_pages *pages, const void *q, const void *k_pages, const void *v_pages,
+                         const int32_t *table, const int32_t *length, const int32_t *count, int32_t n_rows, const uint64_t *sees, void *out,
+                         const int64_t *out_stride, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream) {
   ckv_status st = validate(params);
   if (st != CKV_OK) return st;
   if (!q || !k_pages || !v_pages || !table || !length || !out) return CKV_EINVAL;
@@ -761,10 +760,104 @@ extern "C" ckv_status ckv_paged_attention(const ckv_params *params, const ckv_pa
   if (plan.workgroups > kMostPagedWorkgroups) return CKV_EUNSUPPORTED;
   if (plan.workspace_bytes > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < plan.workspace_bytes))
     return CKV_EWORKSPACE;
-  if (launch_paged_attention(params, s, plan, pages, q, k_pages, v_pages, table, length, count, n_rows, out, out_stride, lse,
+  if (launch_paged_attention(params, s, plan, pages, q, k_pages, v_pages, table, length, count, n_rows, sees, out, out_stride, lse,
                              (char *)workspace, (hipStream_t)hip_stream) != hipSuccess)
     return CKV_EHIP;
   return CKV_OK;
+}
+
+extern "C" ckv_status ckv_paged_attention(const ckv_params *params, const ckv_pages *pages, const void *q, const void *k_pages,
+                                          const void *v_pages, const int32_t *table, const int32_t *length, const int32_t *count,
+                                          int32_t n_rows, void *out, const int64_t *out_stride, float *lse, void *workspace,
+                                          size_t workspace_bytes, void *hip_stream) {
+  return attend(params, pages, q, k_pages, v_pages, table, length, count, n_rows, nullptr, out, out_stride, lse, workspace, workspace_bytes,
+                hip_stream);
+}
+
+extern "C" ckv_status ckv_paged_tree_attention(const ckv_params *params, const ckv_pages *pages, const void *q, const void *k_pages,
+                                               const void *v_pages, const int32_t *table, const int32_t *length, const int32_t *count,
+                                               int32_t n_rows, const uint64_t *sees, void *out, const int64_t *out_stride, float *lse,
+                                               void *workspace, size_t workspace_bytes, void *hip_stream) {
+  if (!sees || ((uintptr_t)sees & 7)) return CKV_EINVAL;
+  if (params && params->seq_len > kMostTreeTokens) return CKV_EUNSUPPORTED;
+  return attend(params, pages, q, k_pages, v_pages, table, length, count, n_rows, sees, out, out_stride, lse, workspace, workspace_bytes,
+                hip_stream);
+}
+
+extern "C" ckv_status ckv_tree_sees(int32_t batch, int32_t n, const int32_t *parent, const int32_t *start, uint64_t *sees, int32_t *positions,
+                                    void *hip_stream) {
+  if (batch < 1 || n < 1 || !parent || !sees || ((uintptr_t)sees & 7) || (positions && !start)) return CKV_EINVAL;
+  if (n > kMostDrafts || (int64_t)batch * n > INT32_MAX / 64) return CKV_EUNSUPPORTED;
+  return launch_tree_sees(batch, n, parent, start, sees, positions, (hipStream_t)hip_stream) == hipSuccess ? CKV_OK : CKV_EHIP;
+}
+
+extern "C" ckv_status ckv_paged_compact(const ckv_params *params, const ckv_pages *pages, const int32_t *table, const int32_t *length,
+                                        const int32_t *count, const int32_t *idx, const int64_t *idx_stride, int32_t cap, const int32_t *kept,
+                                        void *k_pages, void *v_pages, int32_t *length_out, void *hip_stream) {
+  ckv_status st = validate(params);
+  if (st != CKV_OK) return st;
+  if (!table || !length || !idx || !kept || !k_pages || !v_pages || !length_out || length_out == length || cap < 1) return CKV_EINVAL;
+  if (misaligned({k_pages, v_pages})) return CKV_EINVAL;
+  if (idx_stride && (idx_stride[0] < 0 || idx_stride[1] < 0)) return CKV_EINVAL;
+  st = pages_refused(params, pages);
+  if (st != CKV_OK) return st;
+  Shape s;
+  derive(params, &s);
+  if ((int64_t)s.Bz * s.Hkv > INT32_MAX / 1024) return CKV_EUNSUPPORTED;  // workgroups of a launch
+  if (launch_compact(s, pages, table, length, count, idx, idx_stride, cap, kept, k_pages, v_pages, length_out, (hipStream_t)hip_stream) != hipSuccess)
+    return CKV_EHIP;
+  return CKV_OK;
+}
+
+extern "C" ckv_status ckv_pages_copy(const ckv_params *params, const ckv_pages *pages, const int32_t *copy, int32_t n, void *k_pages,
+                                     void *v_pages, void *hip_stream) {
+  ckv_status st = validate(params);
+  if (st != CKV_OK) return st;
+  if (n < 0 || !copy || !k_pages || !v_pages || misaligned({k_pages, v_pages})) return CKV_EINVAL;
+  st = pages_refused(params, pages);
+  if (st != CKV_OK) return st;
+  if (n == 0) return CKV_OK;
+  Shape s;
+  derive(params, &s);
+  if (copy_workgroups(s, pages, n) > kMostPagedWorkgroups) return CKV_EUNSUPPORTED;
+  return launch_pages_copy(s, pages, copy, n, k_pages, v_pages, (hipStream_t)hip_stream) == hipSuccess ? CKV_OK : CKV_EHIP;
+}
+
+static ckv_status lists_refused(const ckv_lists *l) {
+  if (!l || l->batch < 1 || l->n_kv_heads < 1 || l->n_pages < 1 || l->page_rows < 1 || l->max_pages < 1 || l->reserved != 0) return CKV_EINVAL;
+  if (l->table_stride[0] < 0 || l->table_stride[1] < 0) return CKV_EINVAL;
+  const bool own = l->table_stride[1] != 0 && l->n_kv_heads > 1;  // a list for each head
+  if (own && l->table_stride[1] < l->max_pages) return CKV_EINVAL;
+  if (l->batch > 1 && l->table_stride[0] < l->max_pages) return CKV_EINVAL;
+  if (l->page_rows > 65536 || (l->page_rows & (l->page_rows - 1))) return CKV_EUNSUPPORTED;
+  if ((int64_t)l->page_rows * l->max_pages > INT32_MAX) return CKV_EUNSUPPORTED;
+  if ((int64_t)l->batch * l->n_kv_heads > INT32_MAX / l->max_pages) return CKV_EUNSUPPORTED;
+  return CKV_OK;
+}
+
+extern "C" ckv_status ckv_pages_fork(const ckv_lists *lists, const int32_t *table, const int32_t *parent, int32_t *table_out, int32_t *refs,
+                                     uint32_t *taken, const int32_t *length, int32_t *length_out, void *hip_stream) {
+  const ckv_status st = lists_refused(lists);
+  if (st != CKV_OK) return st;
+  if (!table || !parent || !table_out || !refs || !taken || !length != !length_out) return CKV_EINVAL;
+  if (table == table_out || (length && length == length_out)) return CKV_EINVAL;
+  return launch_fork(lists, table, parent, table_out, refs, taken, length, length_out, (hipStream_t)hip_stream) == hipSuccess ? CKV_OK : CKV_EHIP;
+}
+
+extern "C" ckv_status ckv_pages_reserve(const ckv_lists *lists, int32_t *table, const int32_t *first, const int32_t *end, int32_t *refs,
+                                        uint32_t *taken, int32_t *copy, int32_t n_copy, int32_t *result, void *hip_stream) {
+  const ckv_status st = lists_refused(lists);
+  if (st != CKV_OK) return st;
+  if (!table || !first || !end || !refs || !taken || !result || n_copy < 0 || (n_copy > 0 && !copy)) return CKV_EINVAL;
+  return launch_reserve(lists, table, first, end, refs, taken, copy, n_copy, result, (hipStream_t)hip_stream) == hipSuccess ? CKV_OK : CKV_EHIP;
+}
+
+extern "C" ckv_status ckv_pages_free(const ckv_lists *lists, int32_t *table, const int32_t *keep, int32_t *refs, uint32_t *taken,
+                                     void *hip_stream) {
+  const ckv_status st = lists_refused(lists);
+  if (st != CKV_OK) return st;
+  if (!table || !refs || !taken) return CKV_EINVAL;
+  return launch_free(lists, table, keep, refs, taken, (hipStream_t)hip_stream) == hipSuccess ? CKV_OK : CKV_EHIP;
 }
 
 extern "C" const char *ckv_status_string(ckv_status status) {

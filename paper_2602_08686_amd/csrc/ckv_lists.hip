@@ -1,0 +1,313 @@
+// Which lists have which pages: lists that share pages (ckv_pages_fork), get some (ckv_pages_reserve) and give them back (ckv_pages_free).
+//
+// A page's count says how many entries name it, a bit per page whether any does: the free pages are the zero bits, found 32 at a word. What several
+// entries do to a page at once are additions and bits set or cleared, in any order the same; who gets which page goes by the order of the entries.
+#include "ckv_pages.h"
+#include <ckv_dma.h>
+
+namespace ckv {
+
+struct ListArgs {
+  int32_t *table;
+  int64_t table_b, table_h;
+  int32_t *refs;
+  uint32_t *taken;
+  int Hkv, heads, lists;  // heads: lists of a batch element
+  int n_pages, shift, max_pages;
+};
+
+static ListArgs list_args(const ckv_lists *l, int32_t *table, int32_t *refs, uint32_t *taken) {
+  ListArgs a;
+  a.table = table;
+  a.table_b = l->table_stride[0];
+  a.table_h = l->table_stride[1];
+  a.refs = refs;
+  a.taken = taken;
+  a.Hkv = l->n_kv_heads;
+  a.heads = l->table_stride[1] == 0 ? 1 : l->n_kv_heads;
+  a.lists = l->batch * a.heads;
+  a.n_pages = l->n_pages;
+  a.shift = __builtin_ctz((unsigned)l->page_rows);
+  a.max_pages = l->max_pages;
+  return a;
+}
+
+// Atomic at device scope: past the first-level caches.
+template <class T>
+__device__ __forceinline__ T add_across(T *p, T v) { return __scoped_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE); }
+__device__ __forceinline__ void min_across(int32_t *p, int32_t v) { __scoped_atomic_fetch_min(p, v, __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE); }
+__device__ __forceinline__ void take_page(const ListArgs &a, int p) {
+  __scoped_atomic_fetch_or(a.taken + (p >> 5), 1u << (p & 31), __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE);
+}
+__device__ __forceinline__ bool in_pool(const ListArgs &a, int p) { return (unsigned)p < (unsigned)a.n_pages; }
+// One entry less names the page. (A count that says none did keeps saying so.)
+__device__ __forceinline__ void release_page(const ListArgs &a, int p) {
+  const int before = add_across(a.refs + p, -1);
+  if (before == 1) __scoped_atomic_fetch_and(a.taken + (p >> 5), ~(1u << (p & 31)), __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE);
+  else if (before < 1) add_across(a.refs + p, 1);
+}
+__device__ __forceinline__ int32_t *list_of(const ListArgs &a, int l) { return a.table + l / a.heads * a.table_b + l % a.heads * a.table_h; }
+
+constexpr int kEntryThreads = 256;
+
+// ---------------------------------------------------------------------------------------------
+// Lists that become copies
+// ---------------------------------------------------------------------------------------------
+struct ForkArgs {
+  ListArgs to;
+  const int32_t *from;  // strides as to.table
+  const int32_t *parent, *length;
+  int32_t *length_out;
+  int batch, blocks;    // workgroups of a list
+};
+
+// Counts first go up, by the launch in front, and then down, so that a page that stays in use never looks free between.
+template <bool RELEASE>
+__global__ void __launch_bounds__(kEntryThreads) fork_kernel(ForkArgs a) {
+  const int l = blockIdx.x / a.blocks, e = blockIdx.x % a.blocks * kEntryThreads + threadIdx.x, b = l / a.to.heads;
+  const int parent = a.parent[b];
+  const bool goes_on = (unsigned)parent < (unsigned)a.batch;
+  if (RELEASE && a.length_out && blockIdx.x % a.blocks == 0 && l % a.to.heads == 0)
+    for (int g = threadIdx.x; g < a.to.Hkv; g += kEntryThreads) a.length_out[b * a.to.Hkv + g] = goes_on ? a.length[parent * a.to.Hkv + g] : 0;
+  if (e >= a.to.max_pages) return;
+  int32_t *entry = list_of(a.to, l) + e;
+  const int before = *entry;
+  int now = goes_on ? a.from[parent * a.to.table_b + l % a.to.heads * a.to.table_h + e] : -1;
+  if (!in_pool(a.to, now)) now = -1;
+  if (RELEASE) {
+    if (before != now) *entry = now;
+    if (before != now && in_pool(a.to, before)) release_page(a.to, before);
+  } else if (before != now && now >= 0) {
+    if (add_across(a.to.refs + now, 1) == 0) take_page(a.to, now);
+  }
+}
+
+hipError_t launch_fork(const ckv_lists *lists, const int32_t *table, const int32_t *parent, int32_t *table_out, int32_t *refs, uint32_t *taken,
+                       const int32_t *length, int32_t *length_out, hipStream_t stream) {
+  ForkArgs a;
+  a.to = list_args(lists, table_out, refs, taken);
+  a.from = table;
+  a.parent = parent;
+  a.length = length;
+  a.length_out = length_out;
+  a.batch = lists->batch;
+  a.blocks = (lists->max_pages + kEntryThreads - 1) / kEntryThreads;
+  const dim3 grid((unsigned)a.to.lists * a.blocks);
+  hipLaunchKernelGGL(fork_kernel<false>, grid, dim3(kEntryThreads), 0, stream, a);
+  hipLaunchKernelGGL(fork_kernel<true>, grid, dim3(kEntryThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Pages that are given back
+// ---------------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(kEntryThreads) free_kernel(ListArgs a, const int32_t *keep, int blocks) {
+  const int l = blockIdx.x / blocks, e = blockIdx.x % blocks * kEntryThreads + threadIdx.x;
+  int rows = 0;
+  if (keep) {
+    const int32_t *mine = keep + l / a.heads * a.Hkv;
+    if (a.heads > 1) rows = mine[l % a.heads];
+    else
+      for (int g = 0; g < a.Hkv; ++g) rows = max(rows, mine[g]);
+  }
+  const int stay = rows <= 0 ? 0 : ((rows - 1) >> a.shift) + 1;
+  if (e < stay || e >= a.max_pages) return;
+  int32_t *entry = list_of(a, l) + e;
+  const int p = *entry;
+  if (p != -1) *entry = -1;
+  if (in_pool(a, p)) release_page(a, p);
+}
+
+hipError_t launch_free(const ckv_lists *lists, int32_t *table, const int32_t *keep, int32_t *refs, uint32_t *taken, hipStream_t stream) {
+  const ListArgs a = list_args(lists, table, refs, taken);
+  const int blocks = (a.max_pages + kEntryThreads - 1) / kEntryThreads;
+  hipLaunchKernelGGL(free_kernel, dim3((unsigned)a.lists * blocks), dim3(kEntryThreads), 0, stream, a, keep, blocks);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Pages for rows to come
+// ---------------------------------------------------------------------------------------------
+struct ReserveArgs {
+  ListArgs to;
+  const int32_t *first, *end;  // [batch][Hkv]
+  int32_t *copy, *result;
+  int n_copy;
+};
+
+constexpr int kReserveThreads = 1024, kReserveWaves = kReserveThreads / kWave;
+constexpr int kFreeAhead = 2 * kReserveThreads;  // free pages found ahead: a round takes kReserveThreads at most
+
+// One workgroup, its entries in rounds of a thread each, in their order. The entries' pages are counted down by one each; what is left of a page's count
+// are the entries elsewhere. Where none are left, the last entry keeps the page: all write their number into the count, negative, and the
+// smallest stays. Then what is needed is known, and either the counts become what they are to be, or what they were.
+__global__ void __launch_bounds__(kReserveThreads) reserve_kernel(ReserveArgs a) {
+  __shared__ int s_off[kReserveThreads + 1], s_entry[kReserveThreads];  // of the lists: entries in front, the first entry
+  __shared__ int s_sum[kReserveWaves];
+  __shared__ int s_free[kFreeAhead];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+
+  // Sum over the threads in front; `total` of all.
+  auto scan = [&](int x, int &total) CKV_INLINE {
+    const int upto = wave_inclusive(x);
+    __syncthreads();  // the sums have been read
+    if (lane == kWave - 1) s_sum[wave] = upto;
+    __syncthreads();
+    int in_front = 0;
+    total = 0;
+    for (int w = 0; w < kReserveWaves; ++w) {
+      if (w < wave) in_front += s_sum[w];
+      total += s_sum[w];
+    }
+    return in_front + upto - x;
+  };
+  // Calls `visit(entry or null, its number)` for every entry of the ranges, all threads together.
+  auto entries = [&](auto visit) CKV_INLINE {
+    int number = 0;
+    for (int l0 = 0; l0 < a.to.lists; l0 += kReserveThreads) {
+      const int l = l0 + tid;
+      int from = 0, upto = 0;  // rows
+      if (l < a.to.lists) {
+        const int at = l / a.to.heads * a.to.Hkv + (a.to.heads > 1 ? l % a.to.heads : 0);
+        for (int g = 0; g < (a.to.heads > 1 ? 1 : a.to.Hkv); ++g) {
+          const int f = max(a.first[at + g], 0), e = a.end[at + g];
+          if (e <= f) continue;
+          from = upto == 0 ? f : min(from, f);
+          upto = max(upto, e);
+        }
+      }
+      const int e0 = from >> a.to.shift, e1 = upto > 0 ? min(((upto - 1) >> a.to.shift) + 1, a.to.max_pages) : 0;
+      int total;
+      const int off = scan(max(e1 - e0, 0), total);
+      s_off[tid] = off;
+      s_entry[tid] = e0;
+      if (tid == 0) s_off[kReserveThreads] = total;
+      __syncthreads();
+      for (int i0 = 0; i0 < total; i0 += kReserveThreads) {
+        const int i = i0 + tid;
+        int32_t *entry = nullptr;
+        if (i < total) {
+          int lo = 0, hi = kReserveThreads - 1;  // the last list that begins at or in front of i
+          while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (s_off[mid] <= i) lo = mid;
+            else hi = mid - 1;
+          }
+          entry = list_of(a.to, l0 + lo) + s_entry[lo] + i - s_off[lo];
+        }
+        visit(entry, number + i);
+      }
+      number += total;
+      __syncthreads();
+    }
+  };
+  auto done = [&]() CKV_INLINE {  // what all threads have done to the counts is there
+    wait_vm_at_most<0>();
+    __syncthreads();
+  };
+
+  for (int i = tid; i < 2 * a.n_copy; i += kReserveThreads) a.copy[i] = -1;
+  const int words = (a.to.n_pages + 31) / 32;
+  auto free_bits = [&](int w) CKV_INLINE {
+    uint32_t bits = ~a.to.taken[w];
+    if (w == words - 1 && a.to.n_pages % 32) bits &= (1u << a.to.n_pages % 32) - 1u;
+    return bits;
+  };
+  int free = 0;
+  for (int w = tid; w < words; w += kReserveThreads) free += __popc(free_bits(w));
+
+  entries([&](int32_t *entry, int) CKV_INLINE {
+    if (entry && in_pool(a.to, *entry)) add_across(a.to.refs + *entry, -1);
+  });
+  done();
+  entries([&](int32_t *entry, int number) CKV_INLINE {
+    if (entry && in_pool(a.to, *entry) && load_across(a.to.refs + *entry) <= 0) min_across(a.to.refs + *entry, -1 - number);
+  });
+  done();
+  // what an entry needs: nothing (0), a page (1), a page and a copy of the one that it names (2)
+  auto need_of = [&](const int32_t *entry, int number) CKV_INLINE {
+    if (!entry) return 0;
+    if (!in_pool(a.to, *entry)) return 1;
+    return load_across(a.to.refs + *entry) == -1 - number ? 0 : 2;
+  };
+  int need = 0, leave = 0;
+  entries([&](int32_t *entry, int number) CKV_INLINE {
+    const int x = need_of(entry, number);
+    need += x > 0;
+    leave += x == 2;
+  });
+  int all_free, all_need, all_leave;
+  scan(free, all_free);
+  scan(need, all_need);
+  scan(leave, all_leave);
+  const int missing = max(max(all_need - all_free, all_leave - a.n_copy), 0);
+  if (tid == 0) {
+    a.result[0] = missing;
+    a.result[1] = missing ? 0 : all_leave;
+  }
+  if (missing) {
+    entries([&](int32_t *entry, int number) CKV_INLINE {
+      if (entry && in_pool(a.to, *entry) && load_across(a.to.refs + *entry) == -1 - number) store_across(a.to.refs + *entry, 0);
+    });
+    done();
+    entries([&](int32_t *entry, int) CKV_INLINE {
+      if (entry && in_pool(a.to, *entry)) add_across(a.to.refs + *entry, 1);
+    });
+    return;
+  }
+
+  int64_t page = 0;           // free pages in front of it have been found
+  int have = 0, used = 0;     // of s_free
+  int pairs = 0;              // written
+  entries([&](int32_t *entry, int number) CKV_INLINE {
+    const int x = need_of(entry, number);
+    int total;
+    const int at = scan((x > 0) | (x == 2) << 16, total);
+    const int asked = total & 0xffff;
+    if (have - used < asked) {
+      const int left = have - used;
+      const int keep = tid < left ? s_free[used + tid] : 0;  // less than a round's
+      __syncthreads();
+      if (tid < left) s_free[tid] = keep;
+      used = 0;
+      have = left;
+      while (have < asked && page < a.to.n_pages) {
+        const int64_t w0 = page >> 5, w = w0 + tid;
+        uint32_t bits = w < words ? free_bits((int)w) : 0u;
+        if (tid == 0) bits &= ~0u << (page & 31);
+        int found;
+        int to = have + scan(__popc(bits), found);
+        for (; bits && to < kFreeAhead; bits &= bits - 1) s_free[to++] = (int)(w * 32 + __builtin_ctz(bits));
+        __syncthreads();
+        const bool full = have + found >= kFreeAhead;
+        page = full ? (int64_t)s_free[kFreeAhead - 1] + 1 : (w0 + kReserveThreads) * 32;
+        have = full ? kFreeAhead : have + found;
+      }
+    }
+    __syncthreads();
+    if (x > 0 && used + (at & 0xffff) < have) {  // as many were counted, unless somebody else changes the bits meanwhile
+      const int now = s_free[used + (at & 0xffff)];
+      if (x == 2) {
+        const int pair = pairs + (at >> 16);
+        a.copy[2 * (size_t)pair] = *entry;
+        a.copy[2 * (size_t)pair + 1] = now;
+      }
+      *entry = now;
+      store_across(a.to.refs + now, 1);
+      take_page(a.to, now);
+    } else if (entry && x == 0) {
+      store_across(a.to.refs + *entry, 1);
+    }
+    used += asked;
+    pairs += total >> 16;
+  });
+}
+
+hipError_t launch_reserve(const ckv_lists *lists, int32_t *table, const int32_t *first, const int32_t *end, int32_t *refs, uint32_t *taken,
+                          int32_t *copy, int n_copy, int32_t *result, hipStream_t stream) {
+  const ReserveArgs a = {list_args(lists, table, refs, taken), first, end, copy, result, n_copy};
+  hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kReserveThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace ckv

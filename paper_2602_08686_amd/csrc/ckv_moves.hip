@@ -1,0 +1,159 @@
+// Rows that move inside their pages (ckv_paged_compact) and pages that are copied (ckv_pages_copy).
+#include "ckv_pages.h"
+#include <ckv_dma.h>
+
+namespace ckv {
+
+// ---------------------------------------------------------------------------------------------
+// Rows
+// ---------------------------------------------------------------------------------------------
+// In place: row r of the moved ones comes from idx[r] >= r (ascending numbers, none twice), so what is written for r holds no source of a later
+// row, and the sources that it does hold are those of rows up to r. Reads may run ahead of writes as far as they like; a write waits for the
+// reads of its own round and the earlier ones, which a workgroup that takes a list's rows in order has behind a barrier a round. The pieces of a row are
+// independent, so keys, values and parts of rows go to workgroups of their own.
+struct CompactArgs {
+  PageLists lists;  // count null: all rows of a list
+  char *k, *v;
+  const int32_t *idx, *kept;
+  int64_t idx_b, idx_h;
+  int32_t *length_out;
+  int cap, Hkv;
+  int row_pieces;  // of 16 bytes of a row
+  int pieces;      // of a row's keys and values that a workgroup takes: a power of two
+  int splits;      // workgroups of a list
+};
+
+constexpr int kRowsAhead = 4;  // of a thread
+
+__global__ void __launch_bounds__(1024) compact_rows_kernel(CompactArgs a) {
+  const int unit = blockIdx.x / a.splits, slice = blockIdx.x % a.splits, b = unit / a.Hkv, g = unit % a.Hkv;
+  const int length = max(a.lists.length[unit], 0);
+  const int count = a.lists.count ? min(max(a.lists.count[unit], 0), length) : length, first = length - count;
+  const int m = min(max(a.kept[unit], 0), min(count, a.cap));
+  if (slice == 0 && threadIdx.x == 0) a.length_out[unit] = first + m;
+  const int piece = slice * a.pieces + threadIdx.x % a.pieces, rows = blockDim.x / a.pieces, mine = threadIdx.x / a.pieces;
+  const bool values = piece >= a.row_pieces;
+  const int64_t s_page = values ? a.lists.vs[0] : a.lists.ks[0], s_row = values ? a.lists.vs[2] : a.lists.ks[2];
+  char *base = (values ? a.v + g * a.lists.vs[1] : a.k + g * a.lists.ks[1]) + (piece - (values ? a.row_pieces : 0)) * 16;
+  const int32_t *list = a.lists.table + b * a.lists.table_b + g * a.lists.table_h, *idx = a.idx + b * a.idx_b + g * a.idx_h;
+  const int in_page = (1 << a.lists.shift) - 1;
+  for (int r0 = 0; r0 < m; r0 += kRowsAhead * rows) {
+    int from[kRowsAhead], from_page[kRowsAhead], to_page[kRowsAhead];
+    u32x4_d x[kRowsAhead];
+#pragma unroll
+    for (int j = 0; j < kRowsAhead; ++j) {
+      const int r = r0 + j * rows + mine;
+      from[j] = r < m ? idx[r] : -1;
+      if (from[j] < 0 || from[j] >= count || from[j] == r || first + from[j] >= a.lists.capacity || first + r >= a.lists.capacity) from[j] = -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kRowsAhead; ++j) {
+      from_page[j] = to_page[j] = -1;
+      if (from[j] >= 0) {
+        from_page[j] = list[(first + from[j]) >> a.lists.shift];
+        to_page[j] = list[(first + r0 + j * rows + mine) >> a.lists.shift];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kRowsAhead; ++j) {
+      if ((unsigned)from_page[j] >= (unsigned)a.lists.n_pages || (unsigned)to_page[j] >= (unsigned)a.lists.n_pages) from[j] = -1;
+      x[j] = u32x4_d{0u, 0u, 0u, 0u};
+      if (from[j] >= 0) x[j] = *reinterpret_cast<const u32x4_d *>(base + from_page[j] * s_page + ((first + from[j]) & in_page) * s_row);
+    }
+    wait_vm_at_most<0>();
+#pragma unroll
+    for (int j = 0; j < kRowsAhead; ++j) asm volatile("" : "+v"(x[j]));  // read in front of the barrier
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kRowsAhead; ++j)
+      if (from[j] >= 0) *reinterpret_cast<u32x4_d *>(base + to_page[j] * s_page + ((first + r0 + j * rows + mine) & in_page) * s_row) = x[j];
+  }
+}
+
+hipError_t launch_compact(const Shape &s, const ckv_pages *pages, const int32_t *table, const int32_t *length, const int32_t *count,
+                          const int32_t *idx, const int64_t *idx_stride, int cap, const int32_t *kept, void *k_pages, void *v_pages,
+                          int32_t *length_out, hipStream_t stream) {
+  CompactArgs a;
+  a.lists = page_lists(s, pages, table, length, count);
+  a.k = static_cast<char *>(k_pages);
+  a.v = static_cast<char *>(v_pages);
+  a.idx = idx;
+  a.kept = kept;
+  a.idx_b = idx_stride ? idx_stride[0] : (int64_t)s.Hkv * cap;
+  a.idx_h = idx_stride ? idx_stride[1] : cap;
+  a.length_out = length_out;
+  a.cap = cap;
+  a.Hkv = s.Hkv;
+  a.row_pieces = s.d * s.esize / 16;
+  a.splits = (int64_t)cap * 2 * a.row_pieces <= 1024 ? 1 : a.row_pieces / 4;  // parts of 128 bytes
+  a.pieces = 2 * a.row_pieces / a.splits;
+  int threads = 1024;
+  while (threads > 64 && (int64_t)cap * a.pieces <= threads / 2) threads /= 2;
+  hipLaunchKernelGGL(compact_rows_kernel, dim3((unsigned)(s.Bz * s.Hkv * a.splits)), dim3(threads), 0, stream, a);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Pages
+// ---------------------------------------------------------------------------------------------
+struct CopyArgs {
+  char *k, *v;
+  const int32_t *copy;
+  int64_t ks[3], vs[3];  // BYTES between pages, KV heads, rows
+  int n_pages, shift;    // log2(page_rows)
+  int heads, piece_shift;  // log2(pieces of 16 bytes of a row)
+  int total, parts;      // pieces of a pair, keys and values; workgroups of a pair
+};
+constexpr int kCopyThreads = 256, kCopyAhead = 8;
+
+__global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(CopyArgs a) {
+  const int pair = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+  const int src = a.copy[2 * (size_t)pair], dst = a.copy[2 * (size_t)pair + 1];
+  if ((unsigned)src >= (unsigned)a.n_pages || (unsigned)dst >= (unsigned)a.n_pages || src == dst) return;
+  u32x4_d x[kCopyAhead];
+  char *to[kCopyAhead];
+#pragma unroll
+  for (int j = 0; j < kCopyAhead; ++j) {
+    const int64_t at = ((int64_t)part * kCopyAhead + j) * kCopyThreads + threadIdx.x;
+    const int i = (int)(at < a.total ? at : a.total - 1);
+    const int piece = i & ((1 << a.piece_shift) - 1), row = i >> a.piece_shift & ((1 << a.shift) - 1), h = i >> (a.piece_shift + a.shift);
+    const bool values = h >= a.heads;
+    const int64_t in_page = piece * 16 + (values ? (h - a.heads) * a.vs[1] + row * a.vs[2] : h * a.ks[1] + row * a.ks[2]);
+    x[j] = *reinterpret_cast<const u32x4_d *>((values ? a.v + src * a.vs[0] : a.k + src * a.ks[0]) + in_page);
+    to[j] = (values ? a.v + dst * a.vs[0] : a.k + dst * a.ks[0]) + in_page;
+  }
+#pragma unroll
+  for (int j = 0; j < kCopyAhead; ++j)
+    if (((int64_t)part * kCopyAhead + j) * kCopyThreads + threadIdx.x < a.total) *reinterpret_cast<u32x4_d *>(to[j]) = x[j];
+}
+
+// Heads of a page in memory.
+static int heads_of(const Shape &s, const ckv_pages *pages) { return pages->k_stride[1] == 0 && pages->v_stride[1] == 0 ? 1 : s.Hkv; }
+static int64_t pieces_of(const Shape &s, const ckv_pages *pages) {
+  return (int64_t)2 * heads_of(s, pages) * pages->page_rows * (s.d * s.esize / 16);
+}
+int64_t copy_workgroups(const Shape &s, const ckv_pages *pages, int n) {
+  const int64_t pieces = pieces_of(s, pages), each = kCopyThreads * kCopyAhead;
+  return pieces > INT32_MAX ? INT64_MAX : n * ((pieces + each - 1) / each);
+}
+
+hipError_t launch_pages_copy(const Shape &s, const ckv_pages *pages, const int32_t *copy, int n, void *k_pages, void *v_pages, hipStream_t stream) {
+  CopyArgs a;
+  a.k = static_cast<char *>(k_pages);
+  a.v = static_cast<char *>(v_pages);
+  a.copy = copy;
+  for (int i = 0; i < 3; ++i) {
+    a.ks[i] = pages->k_stride[i] * s.esize;
+    a.vs[i] = pages->v_stride[i] * s.esize;
+  }
+  a.n_pages = pages->n_pages;
+  a.shift = __builtin_ctz((unsigned)pages->page_rows);
+  a.heads = heads_of(s, pages);
+  a.piece_shift = __builtin_ctz((unsigned)(s.d * s.esize / 16));
+  a.total = (int)pieces_of(s, pages);
+  a.parts = (int)(copy_workgroups(s, pages, 1));
+  hipLaunchKernelGGL(copy_pages_kernel, dim3((unsigned)copy_workgroups(s, pages, n)), dim3(kCopyThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace ckv

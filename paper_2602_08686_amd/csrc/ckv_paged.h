@@ -1,4 +1,4 @@
-// What the kernels of ckv_paged_attention share (private): the matrix forms of the two products, and how a call is shared out.
+// What the kernels of ckv_paged_attention and ckv_paged_tree_attention share (private): the matrix forms of the two products, and how a call is shared out.
 #ifndef CKV_PAGED_H_
 #define CKV_PAGED_H_
 
@@ -25,6 +25,12 @@ struct PagedArgs {
   float scale2;        // softmax scale * log2(e)
 };
 constexpr int kMostChunks = 64;  // a lane for each
+
+// New tokens that see of one another what a tree of drafts lets them see.
+struct TreeArgs : PagedArgs {
+  const uint32_t *sees;  // [Bz][n][words]: bit t of a token's words: it sees new token t; null: all up to itself (PagedArgs)
+  int words;             // 32-bit words of a token, an even number
+};
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_p;
 typedef __attribute__((ext_vector_type(16))) float f32x16_p;
@@ -84,6 +90,31 @@ __device__ __forceinline__ Column column(const PagedArgs &a, int unit, int tile,
   c.limit = min(max(max(a.lists.length[unit], 0) - new_rows(a.lists, unit, a.n) + c.token + 1, 0), a.n_rows);
   return c;
 }
+
+// Rows that all columns of a wave see whose first one this is: what it sees, or with a tree the rows in front of the new ones.
+__device__ __forceinline__ int every_column_sees(const PagedArgs &, int, const Column &first) { return __builtin_amdgcn_readfirstlane(first.limit); }
+__device__ __forceinline__ int every_column_sees(const TreeArgs &a, int unit, const Column &first) {
+  return __builtin_amdgcn_readfirstlane(min(first.limit, max(a.lists.length[unit], 0) - new_rows(a.lists, unit, a.n)));
+}
+
+// New token of row z_row (less than 0: rows in front of the new ones).
+__device__ __forceinline__ int token_of(const TreeArgs &a, int unit, int z_row) {
+  return z_row - (max(a.lists.length[unit], 0) - new_rows(a.lists, unit, a.n));
+}
+// Which of the 32 rows from z_row on a column sees (a bit each): those in front of the new ones, and of these what its token's words say (word(w) is
+// word w of them) up to itself, which is the last one below its limit.
+template <class Word>
+__device__ __forceinline__ uint32_t rows_of_tree(const TreeArgs &a, int limit, int z_row, int t, Word word) {
+  const int room = limit - z_row;
+  uint32_t seen = room <= 0 ? 0u : room >= 32 ? ~0u : (1u << room) - 1u;
+  if (t > -32) {
+    const int w = t >> 5;
+    const uint32_t lo = w < 0 ? ~0u : w < a.words ? word(w) : 0u, hi = w + 1 < a.words ? word(w + 1) : 0u;
+    seen &= (uint32_t)(((uint64_t)hi << 32 | lo) >> (t & 31));
+  }
+  return seen;
+}
+__device__ __forceinline__ const uint32_t *words_of(const TreeArgs &a, int unit) { return a.sees + (size_t)(unit / a.Hkv) * a.n * a.words; }
 
 // Over the two lanes (l, l ^ 32) that share a column.
 template <class Op>
@@ -359,11 +390,12 @@ __device__ __forceinline__ void store_lse(const PagedArgs &a, int b, const Colum
   if (a.lse) a.lse[((size_t)b * a.Hq + c.h) * a.n + c.token] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
-constexpr int kRowsCols = 32;  // columns of a tile of paged_rows_kernel
+constexpr int kRowsCols = 32;  // columns of a tile of attend_rows
 // Up to here it takes a call's columns, in tiles that read the same rows at the same time. bf16: two tiles (35 columns, 9k rows: 31.3 us with
 // paged_tile_kernel, 30.5, 63 columns 33.2, 32.0; from three tiles on that one reads less). f32, where the products of the matrix cores take longer than the rows: their
 // shares of the rows are what keeps the chip busy (200 columns, 1k rows 17.4 -> 13.1, 256, 2k 40 -> 34, 2048, 4k the other way round).
 constexpr int kMostRowsCols = 64, kMostRowsColsF32 = 256;
+constexpr int kMostRowsWords = 2 * ((kMostRowsColsF32 + 63) / 64);  // of a token of a tree there
 // Columns of a call, and their product with the chunks, up to which a tile's chunks are joined in the launch that makes them: above, leaving and
 // reading the sums past the caches takes one workgroup longer than a kernel of many behind this one takes with them. us, two launches / one: one
 // token, 32/8 heads, 2000 rows 12.7 / 11.3 (4 x 8), batch 4, 32768 rows 86.0 / 84.5, 65000 rows 50.1 / 48.3 (4 x 32), 28/4 heads, batch 8,
@@ -372,6 +404,7 @@ constexpr int kMostRowsCols = 64, kMostRowsColsF32 = 256;
 constexpr int kMostJoinedCols = 16;
 constexpr int kMostJoined = 128;
 void launch_paged_rows(const PagedArgs &a, bool bf16, int d, hipStream_t stream);
+void launch_tree(const TreeArgs &a, const PagedPlan &plan, bool bf16, int d, hipStream_t stream);  // without the merge
 
 }  // namespace ckv
 #endif

@@ -54,8 +54,27 @@ constexpr int64_t kMostPagedWorkgroups = 1 << 22;  // 512 threads of each have t
 PagedPlan plan_paged(const Shape &s, int n_rows);
 hipError_t launch_paged_attention(const ckv_params *p, const Shape &s, const PagedPlan &plan, const ckv_pages *pages, const void *q,
                                   const void *k_pages, const void *v_pages, const int32_t *table, const int32_t *length,
-                                  const int32_t *count, int n_rows, void *out, const int64_t *out_stride, float *lse, char *ws,
-                                  hipStream_t stream);
+                                  const int32_t *count, int n_rows, const uint64_t *sees, void *out, const int64_t *out_stride, float *lse,
+                                  char *ws, hipStream_t stream);
+
+// Trees of drafted tokens.
+constexpr int kMostTreeTokens = 65536;  // a token's words times the tokens stay below 2^31
+constexpr int kMostDrafts = 4096;       // of ckv_tree_sees: a word and a number of each in LDS
+hipError_t launch_tree_sees(int batch, int n, const int32_t *parent, const int32_t *start, uint64_t *sees, int32_t *positions, hipStream_t stream);
+
+// Rows and pages that move.
+hipError_t launch_compact(const Shape &s, const ckv_pages *pages, const int32_t *table, const int32_t *length, const int32_t *count,
+                          const int32_t *idx, const int64_t *idx_stride, int cap, const int32_t *kept, void *k_pages, void *v_pages,
+                          int32_t *length_out, hipStream_t stream);
+int64_t copy_workgroups(const Shape &s, const ckv_pages *pages, int n);
+hipError_t launch_pages_copy(const Shape &s, const ckv_pages *pages, const int32_t *copy, int n, void *k_pages, void *v_pages, hipStream_t stream);
+
+// Which lists have which pages.
+hipError_t launch_fork(const ckv_lists *lists, const int32_t *table, const int32_t *parent, int32_t *table_out, int32_t *refs, uint32_t *taken,
+                       const int32_t *length, int32_t *length_out, hipStream_t stream);
+hipError_t launch_reserve(const ckv_lists *lists, int32_t *table, const int32_t *first, const int32_t *end, int32_t *refs, uint32_t *taken,
+                          int32_t *copy, int n_copy, int32_t *result, hipStream_t stream);
+hipError_t launch_free(const ckv_lists *lists, int32_t *table, const int32_t *keep, int32_t *refs, uint32_t *taken, hipStream_t stream);
 
 }  // namespace ckv
 #endif

@@ -34,7 +34,7 @@ class Struct {
 };
 
 const char *type_name(at::ScalarType t) {
-  return t == at::kInt ? "int32" : t == at::kFloat ? "float32" : "bfloat16";
+  return t == at::kInt ? "int32" : t == at::kLong ? "int64" : t == at::kFloat ? "float32" : "bfloat16";
 }
 
 class Tensors {
@@ -71,6 +71,25 @@ class Tensors {
                       : t->size(1) == p->n_kv_heads && (t->size(1) == 1 || t->stride(1) == g->table_stride[1]));
       if (!ok) refuse("table", at::kInt, {p->batch, p->n_kv_heads, g->max_pages}, "(or without the heads' axis) with the strides that the pages describe");
     }
+  }
+  // Of lists, as the call describes them.
+  void add_list(PyObject *o, const char *name, const ckv_lists *l) {
+    const at::Tensor *t = tensor(o, name);
+    if (!t) return;
+    const bool all = t->dim() == 2;
+    bool ok = t->scalar_type() == at::kInt && (all || t->dim() == 3) && t->size(0) == l->batch && t->size(-1) == l->max_pages;
+    ok = ok && (t->size(-1) == 1 || t->stride(-1) == 1) && (t->size(0) == 1 || t->stride(0) == l->table_stride[0]);
+    ok = ok && (all ? l->n_kv_heads == 1 || l->table_stride[1] == 0
+                    : t->size(1) == l->n_kv_heads && (t->size(1) == 1 || t->stride(1) == l->table_stride[1]));
+    if (!ok) refuse(name, at::kInt, {l->batch, l->n_kv_heads, l->max_pages}, "(or without the heads' axis) with the strides that the lists describe");
+  }
+  // Numbers of rows that stay, one list for all heads of a sequence or one for each: any strides over the axes in front of the last.
+  void add_idx(PyObject *o, const ckv_params *p) {
+    const at::Tensor *t = tensor(o, "idx");
+    if (!t) return;
+    bool ok = t->scalar_type() == at::kInt && (t->dim() == 2 || t->dim() == 3) && t->size(0) == p->batch && t->size(-1) > 0;
+    ok = ok && (t->size(-1) == 1 || t->stride(-1) == 1) && (t->dim() == 2 || t->size(1) == p->n_kv_heads);
+    if (!ok) refuse("idx", at::kInt, {p->batch, p->n_kv_heads, t->dim() > 0 ? t->size(-1) : 0}, "(or without the heads' axis) with a contiguous last axis");
   }
   // Bytes, of any type.
   Py_ssize_t add_bytes(PyObject *o, const char *name) {
@@ -204,9 +223,11 @@ PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// (params, pages, device, q, k_pages, v_pages, table, length, count, out, lse, workspace); behind the addresses the workspace's bytes
+// (params, pages, device, q, k_pages, v_pages, table, length, count, out, lse, workspace), and for trees sees in front of out; behind the
+// addresses the workspace's bytes
+template <bool TREE>
 PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  return checked(n, 12, [&] {
+  return checked(n, 12 + TREE, [&] {
     const Struct<ckv_params> p(a[0]);
     const Struct<ckv_pages> g(a[1]);
     const at::ScalarType type = row_type(p.get());
@@ -216,16 +237,136 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     t.add_table(a[6], p.get(), g.get());
     t.add(a[7], "length", at::kInt, {p->batch, p->n_kv_heads});
     t.add(a[8], "count", at::kInt, {p->batch, p->n_kv_heads});
-    t.add_rows(a[9], "out", type, {p->batch, p->n_q_heads, p->seq_len, p->head_dim});
-    t.add(a[10], "lse", at::kFloat, {p->batch, p->n_q_heads, p->seq_len});
-    const Py_ssize_t bytes = t.add_bytes(a[11], "workspace");
+    if (TREE) t.add(a[9], "sees", at::kLong, {p->batch, p->seq_len, ((int64_t)p->seq_len + 63) / 64});
+    t.add_rows(a[9 + TREE], "out", type, {p->batch, p->n_q_heads, p->seq_len, p->head_dim});
+    t.add(a[10 + TREE], "lse", at::kFloat, {p->batch, p->n_q_heads, p->seq_len});
+    const Py_ssize_t bytes = t.add_bytes(a[11 + TREE], "workspace");
     return t.addresses(bytes);
   });
 }
 
-PyMethodDef methods[] = {{"norm_rotate", (PyCFunction)(void (*)())norm_rotate, METH_FASTCALL, nullptr},
-                         {"paged_append", (PyCFunction)(void (*)())paged_append, METH_FASTCALL, nullptr},
-                         {"paged_attention", (PyCFunction)(void (*)())paged_attention, METH_FASTCALL, nullptr},
+int64_t number(PyObject *o) {
+  const int64_t x = PyLong_AsLongLong(o);
+  if (x == -1 && PyErr_Occurred()) {
+    PyErr_Clear();
+    throw std::invalid_argument("a size is needed");
+  }
+  return x;
+}
+
+// (device, batch, n, parent, start, sees, positions)
+PyObject *tree_sees(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked(n, 7, [&] {
+    const int64_t batch = number(a[1]), tokens = number(a[2]);
+    Tensors t(a[0]);
+    t.add(a[3], "parent", at::kInt, {batch, tokens});
+    t.add(a[4], "start", at::kInt, {batch});
+    t.add(a[5], "sees", at::kLong, {batch, tokens, (tokens + 63) / 64});
+    t.add(a[6], "positions", at::kInt, {batch, tokens});
+    return t.addresses();
+  });
+}
+
+// (params, pages, device, table, length, count, idx, kept, k_pages, v_pages, length_out)
+PyObject *paged_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked(n, 11, [&] {
+    const Struct<ckv_params> p(a[0]);
+    const Struct<ckv_pages> g(a[1]);
+    row_type(p.get());
+    if (!g.get()) throw std::invalid_argument("pages are needed");
+    Tensors t(a[2]);
+    t.add_table(a[3], p.get(), g.get());
+    t.add(a[4], "length", at::kInt, {p->batch, p->n_kv_heads});
+    t.add(a[5], "count", at::kInt, {p->batch, p->n_kv_heads});
+    t.add_idx(a[6], p.get());
+    t.add(a[7], "kept", at::kInt, {p->batch, p->n_kv_heads});
+    add_pools(t, p.get(), g.get(), a[8], a[9]);
+    t.add(a[10], "length_out", at::kInt, {p->batch, p->n_kv_heads});
+    return t.addresses();
+  });
+}
+
+// (params, pages, device, n, copy, k_pages, v_pages)
+PyObject *pages_copy(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked(n, 7, [&] {
+    const Struct<ckv_params> p(a[0]);
+    const Struct<ckv_pages> g(a[1]);
+    row_type(p.get());
+    Tensors t(a[2]);
+    t.add(a[4], "copy", at::kInt, {number(a[3]), 2});
+    add_pools(t, p.get(), g.get(), a[5], a[6]);
+    return t.addresses();
+  });
+}
+
+void add_counts(Tensors &t, const ckv_lists *l, PyObject *refs, PyObject *taken) {
+  t.add(refs, "refs", at::kInt, {l->n_pages});
+  t.add(taken, "taken", at::kInt, {((int64_t)l->n_pages + 31) / 32});
+}
+
+const ckv_lists *needed(const Struct<ckv_lists> &l) {
+  if (!l.get()) throw std::invalid_argument("lists are needed");
+  return l.get();
+}
+
+// (lists, device, table, parent, table_out, refs, taken, length, length_out)
+PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked(n, 9, [&] {
+    const Struct<ckv_lists> held(a[0]);
+    const ckv_lists *l = needed(held);
+    Tensors t(a[1]);
+    t.add_list(a[2], "table", l);
+    t.add(a[3], "parent", at::kInt, {l->batch});
+    t.add_list(a[4], "table_out", l);
+    add_counts(t, l, a[5], a[6]);
+    t.add(a[7], "length", at::kInt, {l->batch, l->n_kv_heads});
+    t.add(a[8], "length_out", at::kInt, {l->batch, l->n_kv_heads});
+    return t.addresses();
+  });
+}
+
+// (lists, device, n_copy, table, first, end, refs, taken, copy, result)
+PyObject *pages_reserve(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked(n, 10, [&] {
+    const Struct<ckv_lists> held(a[0]);
+    const ckv_lists *l = needed(held);
+    Tensors t(a[1]);
+    t.add_list(a[3], "table", l);
+    t.add(a[4], "first", at::kInt, {l->batch, l->n_kv_heads});
+    t.add(a[5], "end", at::kInt, {l->batch, l->n_kv_heads});
+    add_counts(t, l, a[6], a[7]);
+    t.add(a[8], "copy", at::kInt, {number(a[2]), 2});
+    t.add(a[9], "result", at::kInt, {2});
+    return t.addresses();
+  });
+}
+
+// (lists, device, table, keep, refs, taken)
+PyObject *pages_free(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked(n, 6, [&] {
+    const Struct<ckv_lists> held(a[0]);
+    const ckv_lists *l = needed(held);
+    Tensors t(a[1]);
+    t.add_list(a[2], "table", l);
+    t.add(a[3], "keep", at::kInt, {l->batch, l->n_kv_heads});
+    add_counts(t, l, a[4], a[5]);
+    return t.addresses();
+  });
+}
+
+template <class F>
+PyMethodDef method(const char *name, F f) { return {name, (PyCFunction)(void (*)())f, METH_FASTCALL, nullptr}; }
+
+PyMethodDef methods[] = {method("norm_rotate", norm_rotate),
+                         method("paged_append", paged_append),
+                         method("paged_attention", paged_attention<false>),
+                         method("paged_tree_attention", paged_attention<true>),
+                         method("tree_sees", tree_sees),
+                         method("paged_compact", paged_compact),
+                         method("pages_copy", pages_copy),
+                         method("pages_fork", pages_fork),
+                         method("pages_reserve", pages_reserve),
+                         method("pages_free", pages_free),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", "Tensors of the paged cache's calls, checked, and their addresses.", -1, methods};
 
