@@ -61,25 +61,23 @@ struct ForkArgs {
   int batch, blocks;    // workgroups of a list
 };
 
-// Counts first go up, by the launch in front, and then down, so that a page that stays in use never looks free between.
-template <bool RELEASE>
+// A thread for an entry. What it names from now on is counted up, what it named down, in any order: the list that becomes a copy's source still names its
+// pages, so none of them looks free between. One launch: 32 lists of 2048 entries 3.4 us; up and down by a launch each 6.7.
 __global__ void __launch_bounds__(kEntryThreads) fork_kernel(ForkArgs a) {
   const int l = blockIdx.x / a.blocks, e = blockIdx.x % a.blocks * kEntryThreads + threadIdx.x, b = l / a.to.heads;
   const int parent = a.parent[b];
   const bool goes_on = (unsigned)parent < (unsigned)a.batch;
-  if (RELEASE && a.length_out && blockIdx.x % a.blocks == 0 && l % a.to.heads == 0)
+  if (a.length_out && blockIdx.x % a.blocks == 0 && l % a.to.heads == 0)
     for (int g = threadIdx.x; g < a.to.Hkv; g += kEntryThreads) a.length_out[b * a.to.Hkv + g] = goes_on ? a.length[parent * a.to.Hkv + g] : 0;
   if (e >= a.to.max_pages) return;
   int32_t *entry = list_of(a.to, l) + e;
   const int before = *entry;
   int now = goes_on ? a.from[parent * a.to.table_b + l % a.to.heads * a.to.table_h + e] : -1;
   if (!in_pool(a.to, now)) now = -1;
-  if (RELEASE) {
-    if (before != now) *entry = now;
-    if (before != now && in_pool(a.to, before)) release_page(a.to, before);
-  } else if (before != now && now >= 0) {
-    if (add_across(a.to.refs + now, 1) == 0) take_page(a.to, now);
-  }
+  if (before == now) return;
+  *entry = now;
+  if (now >= 0 && add_across(a.to.refs + now, 1) == 0) take_page(a.to, now);
+  if (in_pool(a.to, before)) release_page(a.to, before);
 }
 
 hipError_t launch_fork(const ckv_lists *lists, const int32_t *table, const int32_t *parent, int32_t *table_out, int32_t *refs, uint32_t *taken,
@@ -92,9 +90,7 @@ hipError_t launch_fork(const ckv_lists *lists, const int32_t *table, const int32
   a.length_out = length_out;
   a.batch = lists->batch;
   a.blocks = (lists->max_pages + kEntryThreads - 1) / kEntryThreads;
-  const dim3 grid((unsigned)a.to.lists * a.blocks);
-  hipLaunchKernelGGL(fork_kernel<false>, grid, dim3(kEntryThreads), 0, stream, a);
-  hipLaunchKernelGGL(fork_kernel<true>, grid, dim3(kEntryThreads), 0, stream, a);
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)a.to.lists * a.blocks), dim3(kEntryThreads), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -138,129 +134,99 @@ struct ReserveArgs {
 constexpr int kReserveThreads = 1024, kReserveWaves = kReserveThreads / kWave;
 constexpr int kFreeAhead = 2 * kReserveThreads;  // free pages found ahead: a round takes kReserveThreads at most
 
-// One workgroup, its entries in rounds of a thread each, in their order. The entries' pages are counted down by one each; what is left of a page's count
-// are the entries elsewhere. Where none are left, the last entry keeps the page: all write their number into the count, negative, and the
+// One workgroup, its entries in rounds of a thread each, in their order. Entries whose page others name too count it down by one each; what is left of its
+// count are the entries elsewhere. Where none are left, the last entry keeps the page: all write their number into the count, negative, and the
 // smallest stays. Then what is needed is known, and either the counts become what they are to be, or what they were.
+// A chain of dependent steps: rows, entries, counts, and with shared pages three more of the counts. What can be is asked for beside it (the bits of the
+// first free pages), and a call of one round, which a step's is, keeps its entries in registers: 64 lists of four entries each, no
+// shared page 5 us, 32 lists with one shared page each 7; with all steps for all entries, from memory each time, 15 to 17.
 __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(ReserveArgs a) {
-  __shared__ int s_off[kReserveThreads + 1], s_entry[kReserveThreads];  // of the lists: entries in front, the first entry
-  __shared__ int s_sum[kReserveWaves];
+  __shared__ int s_off[kReserveThreads], s_entry[kReserveThreads];  // of the lists: entries in front, the first entry
+  __shared__ int s_sum[2][kReserveWaves];
   __shared__ int s_free[kFreeAhead];
+  __shared__ int s_shared;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int turn = 0;
 
   // Sum over the threads in front; `total` of all.
   auto scan = [&](int x, int &total) CKV_INLINE {
     const int upto = wave_inclusive(x);
-    __syncthreads();  // the sums have been read
-    if (lane == kWave - 1) s_sum[wave] = upto;
+    int *sums = s_sum[turn ^= 1];  // those of the scan before may still be read
+    if (lane == kWave - 1) sums[wave] = upto;
     __syncthreads();
-    int in_front = 0;
-    total = 0;
-    for (int w = 0; w < kReserveWaves; ++w) {
-      if (w < wave) in_front += s_sum[w];
-      total += s_sum[w];
-    }
-    return in_front + upto - x;
-  };
-  // Calls `visit(entry or null, its number)` for every entry of the ranges, all threads together.
-  auto entries = [&](auto visit) CKV_INLINE {
-    int number = 0;
-    for (int l0 = 0; l0 < a.to.lists; l0 += kReserveThreads) {
-      const int l = l0 + tid;
-      int from = 0, upto = 0;  // rows
-      if (l < a.to.lists) {
-        const int at = l / a.to.heads * a.to.Hkv + (a.to.heads > 1 ? l % a.to.heads : 0);
-        for (int g = 0; g < (a.to.heads > 1 ? 1 : a.to.Hkv); ++g) {
-          const int f = max(a.first[at + g], 0), e = a.end[at + g];
-          if (e <= f) continue;
-          from = upto == 0 ? f : min(from, f);
-          upto = max(upto, e);
-        }
-      }
-      const int e0 = from >> a.to.shift, e1 = upto > 0 ? min(((upto - 1) >> a.to.shift) + 1, a.to.max_pages) : 0;
-      int total;
-      const int off = scan(max(e1 - e0, 0), total);
-      s_off[tid] = off;
-      s_entry[tid] = e0;
-      if (tid == 0) s_off[kReserveThreads] = total;
-      __syncthreads();
-      for (int i0 = 0; i0 < total; i0 += kReserveThreads) {
-        const int i = i0 + tid;
-        int32_t *entry = nullptr;
-        if (i < total) {
-          int lo = 0, hi = kReserveThreads - 1;  // the last list that begins at or in front of i
-          while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (s_off[mid] <= i) lo = mid;
-            else hi = mid - 1;
-          }
-          entry = list_of(a.to, l0 + lo) + s_entry[lo] + i - s_off[lo];
-        }
-        visit(entry, number + i);
-      }
-      number += total;
-      __syncthreads();
-    }
+    const int others = lane < kReserveWaves ? sums[lane] : 0, all = wave_inclusive(others);
+    total = (int)lane_value((uint32_t)all, kWave - 1);
+    return upto - x + (int)lane_value((uint32_t)(all - others), wave);
   };
   auto done = [&]() CKV_INLINE {  // what all threads have done to the counts is there
     wait_vm_at_most<0>();
     __syncthreads();
   };
-
-  for (int i = tid; i < 2 * a.n_copy; i += kReserveThreads) a.copy[i] = -1;
   const int words = (a.to.n_pages + 31) / 32;
-  auto free_bits = [&](int w) CKV_INLINE {
-    uint32_t bits = ~a.to.taken[w];
+  auto free_bits = [&](int64_t w) CKV_INLINE {
+    uint32_t bits = w < words ? ~a.to.taken[w] : 0u;
     if (w == words - 1 && a.to.n_pages % 32) bits &= (1u << a.to.n_pages % 32) - 1u;
     return bits;
   };
-  int free = 0;
-  for (int w = tid; w < words; w += kReserveThreads) free += __popc(free_bits(w));
 
-  entries([&](int32_t *entry, int) CKV_INLINE {
-    if (entry && in_pool(a.to, *entry)) add_across(a.to.refs + *entry, -1);
-  });
-  done();
-  entries([&](int32_t *entry, int number) CKV_INLINE {
-    if (entry && in_pool(a.to, *entry) && load_across(a.to.refs + *entry) <= 0) min_across(a.to.refs + *entry, -1 - number);
-  });
-  done();
-  // what an entry needs: nothing (0), a page (1), a page and a copy of the one that it names (2)
-  auto need_of = [&](const int32_t *entry, int number) CKV_INLINE {
-    if (!entry) return 0;
-    if (!in_pool(a.to, *entry)) return 1;
-    return load_across(a.to.refs + *entry) == -1 - number ? 0 : 2;
+  // The ranges of the lists from l0 on: entries of them all; s_off and s_entry for find().
+  auto ranges = [&](int l0) CKV_INLINE {
+    const int l = l0 + tid;
+    int from = INT32_MAX, upto = 0;  // rows
+    if (l < a.to.lists) {
+      const int heads = a.to.heads > 1 ? 1 : a.to.Hkv, at = l / a.to.heads * a.to.Hkv + l % a.to.heads;
+#pragma unroll 8
+      for (int g = 0; g < heads; ++g) {
+        const int f = max(a.first[at + g], 0), e = a.end[at + g];
+        from = min(from, e > f ? f : INT32_MAX);
+        upto = max(upto, e > f ? e : 0);
+      }
+    }
+    const int e0 = from >> a.to.shift, e1 = upto > 0 ? min(((upto - 1) >> a.to.shift) + 1, a.to.max_pages) : 0;
+    int total;
+    s_off[tid] = scan(max(e1 - e0, 0), total);
+    s_entry[tid] = e0;
+    __syncthreads();
+    return total;
   };
-  int need = 0, leave = 0;
-  entries([&](int32_t *entry, int number) CKV_INLINE {
-    const int x = need_of(entry, number);
-    need += x > 0;
-    leave += x == 2;
-  });
-  int all_free, all_need, all_leave;
-  scan(free, all_free);
-  scan(need, all_need);
-  scan(leave, all_leave);
-  const int missing = max(max(all_need - all_free, all_leave - a.n_copy), 0);
-  if (tid == 0) {
-    a.result[0] = missing;
-    a.result[1] = missing ? 0 : all_leave;
-  }
-  if (missing) {
-    entries([&](int32_t *entry, int number) CKV_INLINE {
-      if (entry && in_pool(a.to, *entry) && load_across(a.to.refs + *entry) == -1 - number) store_across(a.to.refs + *entry, 0);
-    });
-    done();
-    entries([&](int32_t *entry, int) CKV_INLINE {
-      if (entry && in_pool(a.to, *entry)) add_across(a.to.refs + *entry, 1);
-    });
-    return;
-  }
+  auto find = [&](int l0, int i) CKV_INLINE {  // entry i of these ranges
+    int lo = 0, hi = min(a.to.lists - l0, kReserveThreads) - 1;  // the last list that begins at or in front of i
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (s_off[mid] <= i) lo = mid;
+      else hi = mid - 1;
+    }
+    return list_of(a.to, l0 + lo) + s_entry[lo] + i - s_off[lo];
+  };
 
-  int64_t page = 0;           // free pages in front of it have been found
-  int have = 0, used = 0;     // of s_free
-  int pairs = 0;              // written
-  entries([&](int32_t *entry, int number) CKV_INLINE {
-    const int x = need_of(entry, number);
+  // The first free pages, and how many there are.
+  int64_t page = 0;        // free pages in front of it have been found
+  int have = 0, used = 0;  // of s_free
+  auto more_free = [&](uint32_t bits) CKV_INLINE {  // of the words from page / 32 on, a thread each
+    const int64_t w = (page >> 5) + tid;
+    int found;
+    int to = have + scan(__popc(bits), found);
+    for (; bits && to < kFreeAhead; bits &= bits - 1) s_free[to++] = (int)(w * 32 + __builtin_ctz(bits));
+    __syncthreads();
+    const bool full = have + found >= kFreeAhead;
+    page = full ? (int64_t)s_free[kFreeAhead - 1] + 1 : ((page >> 5) + kReserveThreads) * 32;
+    have = full ? kFreeAhead : have + found;
+    return found;
+  };
+  const uint32_t first_bits = free_bits(tid);
+  for (int i = tid; i < 2 * a.n_copy; i += kReserveThreads) a.copy[i] = -1;
+  if (tid == 0) s_shared = 0;
+  const int lists_entries = ranges(0);
+  int all_free = more_free(first_bits);
+  if (words > kReserveThreads) {
+    int rest = 0, sum;
+    for (int64_t w = kReserveThreads + tid; w < words; w += kReserveThreads) rest += __popc(free_bits(w));
+    scan(rest, sum);
+    all_free += sum;
+  }
+  // What a round needs: gives x > 0 its page, x = 2 a pair too. All threads together.
+  int pairs = 0;  // written
+  auto give = [&](int32_t *entry, int was, int x) CKV_INLINE {
     int total;
     const int at = scan((x > 0) | (x == 2) << 16, total);
     const int asked = total & 0xffff;
@@ -272,34 +238,114 @@ __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(ReserveArgs a)
       used = 0;
       have = left;
       while (have < asked && page < a.to.n_pages) {
-        const int64_t w0 = page >> 5, w = w0 + tid;
-        uint32_t bits = w < words ? free_bits((int)w) : 0u;
+        uint32_t bits = free_bits((page >> 5) + tid);
         if (tid == 0) bits &= ~0u << (page & 31);
-        int found;
-        int to = have + scan(__popc(bits), found);
-        for (; bits && to < kFreeAhead; bits &= bits - 1) s_free[to++] = (int)(w * 32 + __builtin_ctz(bits));
-        __syncthreads();
-        const bool full = have + found >= kFreeAhead;
-        page = full ? (int64_t)s_free[kFreeAhead - 1] + 1 : (w0 + kReserveThreads) * 32;
-        have = full ? kFreeAhead : have + found;
+        more_free(bits);
       }
     }
-    __syncthreads();
     if (x > 0 && used + (at & 0xffff) < have) {  // as many were counted, unless somebody else changes the bits meanwhile
       const int now = s_free[used + (at & 0xffff)];
       if (x == 2) {
         const int pair = pairs + (at >> 16);
-        a.copy[2 * (size_t)pair] = *entry;
+        a.copy[2 * (size_t)pair] = was;
         a.copy[2 * (size_t)pair + 1] = now;
       }
       *entry = now;
       store_across(a.to.refs + now, 1);
       take_page(a.to, now);
-    } else if (entry && x == 0) {
-      store_across(a.to.refs + *entry, 1);
     }
     used += asked;
     pairs += total >> 16;
+  };
+  auto result = [&](int need, int leave) CKV_INLINE {  // whether there is enough
+    const int missing = max(max(need - all_free, leave - a.n_copy), 0);
+    if (tid == 0) {
+      a.result[0] = missing;
+      a.result[1] = missing ? 0 : leave;
+    }
+    return missing == 0;
+  };
+  auto shared = [&](int p) CKV_INLINE { return in_pool(a.to, p) && load_across(a.to.refs + p) > 1; };
+
+  if (a.to.lists <= kReserveThreads && lists_entries <= kReserveThreads) {
+    int32_t *entry = tid < lists_entries ? find(0, tid) : nullptr;
+    const int p = entry ? *entry : -1;
+    int x = entry && !in_pool(a.to, p) ? 1 : 0;  // what the entry needs: nothing, a page (1), a page and a copy of the one that it names (2)
+    bool keeps = false;                          // a page that all others leave
+    const bool is_shared = entry && shared(p);
+    if (is_shared) s_shared = 1;
+    __syncthreads();
+    if (s_shared) {
+      if (is_shared) add_across(a.to.refs + p, -1);
+      done();
+      if (is_shared && load_across(a.to.refs + p) <= 0) min_across(a.to.refs + p, -1 - tid);
+      done();
+      if (is_shared) keeps = load_across(a.to.refs + p) == -1 - tid;
+      if (is_shared && !keeps) x = 2;
+    }
+    int total;
+    scan((x > 0) | (x == 2) << 16, total);
+    if (result(total & 0xffff, total >> 16)) {
+      if (keeps) store_across(a.to.refs + p, 1);
+      give(entry, p, x);
+    } else if (s_shared) {
+      if (keeps) store_across(a.to.refs + p, 0);
+      done();
+      if (is_shared) add_across(a.to.refs + p, 1);
+    }
+    return;
+  }
+
+  // Calls `visit(entry or null, its number)` for every entry of the ranges, all threads together.
+  auto entries = [&](auto visit) CKV_INLINE {
+    int number = 0;
+    for (int l0 = 0; l0 < a.to.lists; l0 += kReserveThreads) {
+      const int total = ranges(l0);
+      for (int i0 = 0; i0 < total; i0 += kReserveThreads) {
+        const int i = i0 + tid;
+        visit(i < total ? find(l0, i) : nullptr, number + i);
+      }
+      number += total;
+      __syncthreads();
+    }
+  };
+  // Counts above one are those of shared pages until they are counted down; then those that entries number, negative, are. So all entries are counted
+  // down here, and whoever keeps a page counts it up again.
+  entries([&](int32_t *entry, int) CKV_INLINE {
+    if (entry && in_pool(a.to, *entry)) add_across(a.to.refs + *entry, -1);
+  });
+  done();
+  entries([&](int32_t *entry, int number) CKV_INLINE {
+    if (entry && in_pool(a.to, *entry) && load_across(a.to.refs + *entry) <= 0) min_across(a.to.refs + *entry, -1 - number);
+  });
+  done();
+  auto need_of = [&](const int32_t *entry, int number) CKV_INLINE {
+    if (!entry) return 0;
+    if (!in_pool(a.to, *entry)) return 1;
+    return load_across(a.to.refs + *entry) == -1 - number ? 0 : 2;
+  };
+  int need = 0, leave = 0, all_need, all_leave;
+  entries([&](int32_t *entry, int number) CKV_INLINE {
+    const int x = need_of(entry, number);
+    need += x > 0;
+    leave += x == 2;
+  });
+  scan(need, all_need);
+  scan(leave, all_leave);
+  if (!result(all_need, all_leave)) {
+    entries([&](int32_t *entry, int number) CKV_INLINE {
+      if (entry && in_pool(a.to, *entry) && load_across(a.to.refs + *entry) == -1 - number) store_across(a.to.refs + *entry, 0);
+    });
+    done();
+    entries([&](int32_t *entry, int) CKV_INLINE {
+      if (entry && in_pool(a.to, *entry)) add_across(a.to.refs + *entry, 1);
+    });
+    return;
+  }
+  entries([&](int32_t *entry, int number) CKV_INLINE {
+    const int x = need_of(entry, number), was = entry ? *entry : -1;
+    if (entry && x == 0) store_across(a.to.refs + was, 1);
+    give(entry, was, x);
   });
 }
 

@@ -91,18 +91,12 @@ __device__ __forceinline__ Column column(const PagedArgs &a, int unit, int tile,
   return c;
 }
 
-// Rows that all columns of a wave see whose first one this is: what it sees, or with a tree the rows in front of the new ones.
-__device__ __forceinline__ int every_column_sees(const PagedArgs &, int, const Column &first) { return __builtin_amdgcn_readfirstlane(first.limit); }
-__device__ __forceinline__ int every_column_sees(const TreeArgs &a, int unit, const Column &first) {
-  return __builtin_amdgcn_readfirstlane(min(first.limit, max(a.lists.length[unit], 0) - new_rows(a.lists, unit, a.n)));
-}
-
-// New token of row z_row (less than 0: rows in front of the new ones).
-__device__ __forceinline__ int token_of(const TreeArgs &a, int unit, int z_row) {
-  return z_row - (max(a.lists.length[unit], 0) - new_rows(a.lists, unit, a.n));
+// Row of the first new token. (Read once: in a sweep it would be read from memory again and again.)
+__device__ __forceinline__ int first_new(const PagedArgs &a, int unit) {
+  return __builtin_amdgcn_readfirstlane(max(a.lists.length[unit], 0) - new_rows(a.lists, unit, a.n));
 }
 // Which of the 32 rows from z_row on a column sees (a bit each): those in front of the new ones, and of these what its token's words say (word(w) is
-// word w of them) up to itself, which is the last one below its limit.
+// word w of them) up to itself, which is the last one below its limit. t: new token of row z_row (below 0: in front of them).
 template <class Word>
 __device__ __forceinline__ uint32_t rows_of_tree(const TreeArgs &a, int limit, int z_row, int t, Word word) {
   const int room = limit - z_row;

@@ -70,7 +70,8 @@ __device__ __forceinline__ void attend_rows(const Args &a) {
 
   const bool valid = m < range.cols;
   const Column c = column(a, unit, tile, valid ? m : 0);
-  const int sees_least = every_column_sees(a, unit, c);
+  const int start = TREE ? first_new(a, unit) : 0, sees_first = __builtin_amdgcn_readfirstlane(c.limit);
+  const int sees_least = TREE ? min(sees_first, start) : sees_first;
   if constexpr (TREE) {  // a wave's own copy: here when its first rows are
     const uint32_t *own = words_of(a, unit) + (size_t)c.token * a.words + half;
     for (int j = 0; 2 * j < a.words; ++j) dma_4(own + 2 * j, s_sees[wave] + j * kWave);
@@ -141,7 +142,7 @@ __device__ __forceinline__ void attend_rows(const Args &a) {
       if (missing || (block + 1) * 32 > sees_least) {
         if constexpr (TREE) {
           const auto word = [&](int w) CKV_INLINE { return s_sees[wave][(w >> 1) * kWave + (w & 1) * 32 + m]; };
-          const uint32_t seen = rows_of_tree(a, c.limit, block * 32, token_of(a, unit, block * 32), word) & ~missing;
+          const uint32_t seen = rows_of_tree(a, c.limit, block * 32, block * 32 - start, word) & ~missing;
           const uint32_t own = seen >> (4 * half);
 #pragma unroll
           for (int r = 0; r < 16; ++r)

@@ -96,6 +96,7 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
   };
   __shared__ Offsets s_at[4][kStageRows];
   __shared__ int s_missing, s_undefined;
+  __shared__ __align__(256) uint32_t s_sees[TREE ? WAVES : 1][2][TREE ? 2 * kWave : 1];
 
   // The longest tiles first, of all lists; the lists side by side, so that with a multiple of eight of them a list's workgroups share an L2.
   const int units = a.workgroups / a.col_tiles / a.n_chunks;
@@ -112,7 +113,9 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
   const int local = wave * 32 + (lane & 31);
   const bool valid = local < range.cols;
   const Column c = column(a, unit, tile, valid ? local : 0);
-  const int sees_least = every_column_sees(a, unit, c);  // the wave's first column sees the fewest rows
+  const int start = TREE ? first_new(a, unit) : 0;
+  const int sees_first = __builtin_amdgcn_readfirstlane(c.limit);  // the wave's first column sees the fewest rows
+  const int sees_least = TREE ? min(sees_first, start) : sees_first;  // of a tree those in front of the new ones
   // The wave is through behind the rows that its own columns see.
   const int sees_most = wave * 32 < range.cols ? column(a, unit, tile, min(range.cols, wave * 32 + 32) - 1).limit : 0;
   const int own_last = max(min(last, (sees_most + kStageRows - 1) / kStageRows), first + 1);
@@ -153,6 +156,18 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
     }
   };
 
+  // A wave's columns' words of the rows that it hides in a stage, from 32 rows in front of it on: three words, a stage ahead, two of each
+  // column and then the third.
+  auto fetch_sees = [&](int stage) CKV_INLINE {
+    if constexpr (TREE) {
+      const int w = (stage * kStageRows - 32 - start) >> 5;
+      if (w + 2 < 0 || w >= a.words) return;  // the same for all lanes
+      const uint32_t *own = words_of(a, unit) + (size_t)c.token * a.words;
+      dma_4(own + min(max(w + half, 0), a.words - 1), s_sees[wave][stage & 1]);
+      dma_4(own + min(w + 2, a.words - 1), s_sees[wave][stage & 1] + kWave);
+    }
+  };
+
   Running run;
   f32x16_p acc[I::DTILES];
   auto begin = [&]() CKV_INLINE {
@@ -162,8 +177,8 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[t][r] = 0.0f;
   };
-  // logits of rows that the column does not see
-  auto hide = [&](f32x16_p &z, int z_row) CKV_INLINE {
+  // logits of rows that the column does not see; `stage`: whose words are there, or -1
+  auto hide = [&](f32x16_p &z, int z_row, int stage) CKV_INLINE {
     if (!s_missing && z_row + 32 <= sees_least) return;
     const int sees = c.limit - z_row - 4 * half;  // rows of the block from the half's first one on
     uint32_t there = ~0u;
@@ -176,8 +191,11 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
       }
     }
     if constexpr (TREE) {
-      const auto word = [&](int w) CKV_INLINE { return words_of(a, unit)[(size_t)c.token * a.words + w]; };
-      const uint32_t seen = rows_of_tree(a, c.limit, z_row, token_of(a, unit, z_row), word) >> (4 * half);
+      const auto word = [&](int w) CKV_INLINE {
+        if (stage < 0) return words_of(a, unit)[(size_t)c.token * a.words + w];
+        return s_sees[wave][stage & 1][(w - ((stage * kStageRows - 32 - start) >> 5)) * 32 + (lane & 31)];
+      };
+      const uint32_t seen = rows_of_tree(a, c.limit, z_row, z_row - start, word) >> (4 * half);
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (!(seen >> block_row(r, 0) & 1) || !(there >> r & 1)) z[r] = -INFINITY;
@@ -199,6 +217,7 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
     }
     fetch_ids(first + 2);
     fetch_k(first);
+    fetch_sees(first);
     f32x16_p z;           // logits of the block in work
     Weights<DT> weights;  // of the one before
     // Steps of the pipeline: the first product of a block, the softmax of the one before, the second product of the one before that, none
@@ -208,9 +227,9 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
       to_weights<false>(z, a.scale2, run, kFinite);
       weights = as_operand<DT>(z);
     };
-    auto step = [&](const char *k_image, int z_row, const char *v_image) CKV_INLINE {
+    auto step = [&](const char *k_image, int z_row, const char *v_image, int stage) CKV_INLINE {
       rescale(acc, run);
-      hide(z, z_row);
+      hide(z, z_row, stage);
       f32x16_p next;
       if constexpr (DT == CKV_BF16) {
         whole_step<DT, DH>(k_image, v_image, lane, qf, z, next, weights, acc, a.scale2, run);
@@ -229,11 +248,12 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
       if (stage < last) fetch_v(stage);
       if (stage + 1 < last) fetch_k(stage + 1);
       if (stage + 3 < last) fetch_ids(stage + 3);
+      if (stage + 1 <= last) fetch_sees(stage + 1);
     };
     f32x16_p next;
     advance(first);
     first_product<DT, DH>(s_k[0], lane, qf, z);
-    hide(z, first * kStageRows);
+    hide(z, first * kStageRows, first);
     first_product<DT, DH>(s_k[0] + HALF, lane, qf, next);
     softmax();
     z = next;
@@ -241,8 +261,8 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
     auto stage_of = [&](auto parity, int stage) CKV_INLINE {
       constexpr int BUF = decltype(parity)::value;
       advance(stage);
-      step(s_k[BUF], stage * kStageRows - 32, s_v[BUF ^ 1]);
-      step(s_k[BUF] + HALF, stage * kStageRows, s_v[BUF ^ 1] + HALF);
+      step(s_k[BUF], stage * kStageRows - 32, s_v[BUF ^ 1], stage);
+      step(s_k[BUF] + HALF, stage * kStageRows, s_v[BUF ^ 1] + HALF, stage);
     };
     int stage = first + 1;
 #pragma unroll 1
@@ -255,7 +275,7 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
     const char *v = s_v[(own_last - 1 - first) & 1];
     rescale(acc, run);
     second_product<DT, DH, false>(v, lane, weights, acc, kFinite);
-    hide(z, own_last * kStageRows - 32);
+    hide(z, own_last * kStageRows - 32, own_last);
     softmax();
     rescale(acc, run);
     second_product<DT, DH, false>(v + HALF, lane, weights, acc, kFinite);
@@ -284,7 +304,7 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
         for (int k = 0; k < 2; ++k) {
           f32x16_p z;
           first_product<DT, DH>(s_k[(stage - first) & 1] + k * HALF, lane, qf, z);
-          hide(z, stage * kStageRows + 32 * k);
+          hide(z, stage * kStageRows + 32 * k, -1);
           to_weights<true>(z, a.scale2, run, mode, room);
           if (mode == kFinite) rescale(acc, run);  // marks are counted, whatever the row behind them weighs
           second_product<DT, DH, true>(s_v[(stage - first) & 1] + k * HALF, lane, as_operand<DT>(z), acc, mode);
