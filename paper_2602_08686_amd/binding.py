@@ -432,12 +432,9 @@ def ckv_paged_attention(params, pages, q, k_pages, v_pages, table, length, n_row
 def ckv_tree_sees(parent, start, sees, positions=None, stream=None):
     """parent [batch,n] int32; start [batch] int32; sees [batch,n,ceil(n/64)] int64, a bit for each token that is seen; positions [batch,n]
     int32 or None (start then may be None, too)."""
-    if not isinstance(parent, torch.Tensor) or parent.dim() != 2:
-        raise ValueError("parent has to be int32 [batch,n] contiguous")
-    batch, n = parent.shape
     device, stream = _place(stream)
-    at = load_tensors().tree_sees(device, batch, n, parent, start, sees, positions)
-    _check(load().ckv_tree_sees(batch, n, *at, stream), "ckv_tree_sees")
+    at = load_tensors().tree_sees(device, parent, start, sees, positions)
+    _check(load().ckv_tree_sees(*at, stream), "ckv_tree_sees")
 
 
 def ckv_paged_tree_attention(params, pages, q, k_pages, v_pages, table, length, n_rows, sees, out, lse=None, workspace=None, count=None,
@@ -461,24 +458,17 @@ def pool_params(k_pages: torch.Tensor, table: torch.Tensor) -> CkvParams:
 
 def ckv_paged_compact(params, pages, k_pages, v_pages, table, length, idx, kept, length_out, count=None, stream=None):
     """idx [Bz,cap] (one for all heads) or [Bz,Hkv,cap] int32, any strides with a contiguous last axis; kept, length_out [Bz,Hkv] int32."""
-    if not isinstance(idx, torch.Tensor) or idx.dim() not in (2, 3):
-        raise ValueError("idx has to be int32 [Bz,cap] or [Bz,Hkv,cap] with a contiguous last axis")
-    strides = (ctypes.c_int64 * 2)(idx.stride(0), idx.stride(1) if idx.dim() == 3 else 0)
     device, stream = _place(stream)
-    table_at, length_at, count_at, idx_at, *rest = load_tensors().paged_compact(params, pages, device, table, length, count, idx, kept, k_pages,
-                                                                                v_pages, length_out)
-    _check(load().ckv_paged_compact(ctypes.byref(params), ctypes.byref(pages), table_at, length_at, count_at, idx_at, strides, idx.shape[-1],
-                                    *rest, stream), "ckv_paged_compact")
+    at = load_tensors().paged_compact(params, pages, device, table, length, count, idx, kept, k_pages, v_pages, length_out)
+    _check(load().ckv_paged_compact(ctypes.byref(params), ctypes.byref(pages), *at, stream), "ckv_paged_compact")
 
 
 def ckv_pages_copy(params, pages, k_pages, v_pages, copy, stream=None):
     """copy [n,2] int32: pairs (from, to)."""
-    if not isinstance(copy, torch.Tensor) or copy.dim() != 2:
-        raise ValueError("copy has to be int32 [n,2] contiguous")
     device, stream = _place(stream)
-    copy_at, *pools = load_tensors().pages_copy(params, pages, device, copy.shape[0], copy, k_pages, v_pages)
-    if copy.shape[0]:
-        _check(load().ckv_pages_copy(ctypes.byref(params), ctypes.byref(pages), copy_at, copy.shape[0], *pools, stream), "ckv_pages_copy")
+    at = load_tensors().pages_copy(params, pages, device, copy, k_pages, v_pages)
+    if at[1]:
+        _check(load().ckv_pages_copy(ctypes.byref(params), ctypes.byref(pages), *at, stream), "ckv_pages_copy")
 
 
 def lists_for(table: torch.Tensor, *, n_kv_heads, n_pages, page_rows) -> CkvLists:
@@ -507,10 +497,9 @@ def ckv_pages_fork(lists, table, parent, table_out, refs, taken, length=None, le
 
 def ckv_pages_reserve(lists, table, first, end, refs, taken, copy, result, stream=None):
     """first, end [Bz,Hkv] int32; copy [n,2] int32 or None; result [2] int32."""
-    n = 0 if copy is None else copy.shape[0]
     device, stream = _place(stream)
-    *at, copy_at, result_at = load_tensors().pages_reserve(lists, device, n, table, first, end, refs, taken, copy, result)
-    _check(load().ckv_pages_reserve(ctypes.byref(lists), *at, copy_at, n, result_at, stream), "ckv_pages_reserve")
+    at = load_tensors().pages_reserve(lists, device, table, first, end, refs, taken, copy, result)
+    _check(load().ckv_pages_reserve(ctypes.byref(lists), *at, stream), "ckv_pages_reserve")
 
 
 def ckv_pages_free(lists, table, keep, refs, taken, stream=None):

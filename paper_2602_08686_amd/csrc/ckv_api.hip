@@ -734,8 +734,12 @@ extern "C" size_t ckv_paged_workspace_bytes(const ckv_params *params, int32_t n_
   if (validate(params) != CKV_OK || paged_size_refused(n_rows) != CKV_OK) return 0;
   Shape s;
   derive(params, &s);
-  const PagedPlan plan = plan_paged(s, n_rows);
-  return plan.workgroups > kMostPagedWorkgroups ? 0 : align256(plan.workspace_bytes);
+  size_t most = 0;  // of a call with or without a tree
+  for (const bool tree : {false, true}) {
+    const PagedPlan plan = plan_paged(s, n_rows, tree);
+    if (plan.workgroups <= kMostPagedWorkgroups && plan.workspace_bytes > most) most = plan.workspace_bytes;
+  }
+  return align256(most);
 }
 
 static ckv_status attend(const ckv_params *params, const ckv_pages *pages, const void *q, const void *k_pages, const void *v_pages,
@@ -756,7 +760,7 @@ static ckv_status attend(const ckv_params *params, const ckv_pages *pages, const
   }
   Shape s;
   derive(params, &s);
-  const PagedPlan plan = plan_paged(s, n_rows);
+  const PagedPlan plan = plan_paged(s, n_rows, sees != nullptr);
   if (plan.workgroups > kMostPagedWorkgroups) return CKV_EUNSUPPORTED;
   if (plan.workspace_bytes > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < plan.workspace_bytes))
     return CKV_EWORKSPACE;

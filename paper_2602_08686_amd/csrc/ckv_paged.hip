@@ -2,15 +2,17 @@
 // what workgroups along the rows leave, and how a call is shared out.
 #include "ckv_paged_tile.h"
 
+#include <algorithm>
+
 namespace ckv {
 
 template <int DT, int DH, int WAVES>
 __global__ void __launch_bounds__(WAVES *kWave, tile_occupancy(DT, DH, WAVES)) paged_tile_kernel(PagedArgs a) {
-  attend_tile<DT, DH, WAVES>(a);
+  attend_tile<DT, DH, WAVES, 1>(a);
 }
 
 // Chunks of a column, in their order. A column's lanes take four components each, and for the weights a chunk each; loads of eight chunks are in flight
-// together (one after the other, sixteen chunks took 12 us, now 5).
+// together (one after the other, sixteen chunks took 12 us, now 5), the first ones beside those for the weights.
 constexpr int kMergeThreads = 256;
 template <int DT, int DH>
 __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a) {
@@ -22,6 +24,15 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a)
   const TileRange range = tile_range(a, unit, tile);
   const int chunks = valid ? (range.stages + range.per_chunk - 1) / range.per_chunk : 0;
   const size_t first = ((size_t)unit * a.col_tiles + tile) * a.n_chunks * a.tile_cols + local;
+  constexpr int BATCH = 8;
+  f32x4_p x[BATCH];
+  const auto fetch = [&](int i0) CKV_INLINE {
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      x[j] = f32x4_p{0.0f, 0.0f, 0.0f, 0.0f};
+      if (i0 + j < chunks) x[j] = *reinterpret_cast<const f32x4_p *>(a.part + (first + (size_t)(i0 + j) * a.tile_cols) * DH + 4 * piece);
+    }
+  };
   float2 st[SHARE];
   float top = -INFINITY;
 #pragma unroll
@@ -29,8 +40,10 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a)
     const int i = k * PIECES + piece;
     st[k] = make_float2(-INFINITY, 0.0f);
     if (i < chunks) st[k] = a.stats[first + (size_t)i * a.tile_cols];
-    top = fmaxf(top, st[k].x);
   }
+  fetch(0);
+#pragma unroll
+  for (int k = 0; k < SHARE; ++k) top = fmaxf(top, st[k].x);
 #pragma unroll
   for (int o = 1; o < PIECES; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
   const float ref = top == -INFINITY ? 0.0f : top;
@@ -46,17 +59,10 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a)
 #pragma unroll
   for (int k = 0; k < SHARE; ++k) weight[k] *= inv;
   f32x4_p num = {0.0f, 0.0f, 0.0f, 0.0f};
-  constexpr int BATCH = 8;
 #pragma unroll
   for (int k = 0; k < SHARE; ++k) {
     for (int c0 = 0; c0 < PIECES && k * PIECES + c0 < a.n_chunks; c0 += BATCH) {  // the same for all lanes
-      f32x4_p x[BATCH];
-#pragma unroll
-      for (int j = 0; j < BATCH; ++j) {
-        const int i = k * PIECES + c0 + j;
-        x[j] = f32x4_p{0.0f, 0.0f, 0.0f, 0.0f};
-        if (i < chunks) x[j] = *reinterpret_cast<const f32x4_p *>(a.part + (first + (size_t)i * a.tile_cols) * DH + 4 * piece);
-      }
+      if (k > 0 || c0 > 0) fetch(k * PIECES + c0);
 #pragma unroll
       for (int j = 0; j < BATCH; ++j) num = add_part(num, x[j], __shfl(weight[k], (threadIdx.x & 63) / PIECES * PIECES + c0 + j));
     }
@@ -81,12 +87,20 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a)
 // themselves 24.1 / 19.5 / 19.5; f32, heads of 64, 101 tokens, 523 rows (64 / 128) 24.3 / 29.6. One chunk up to 1024 (bf16) or 256 (f32) rows
 // of few columns: 500 rows 10.1, two chunks 11.0; batch 16, 544 rows 10.7, two chunks 11.6, 1000 rows 16.9, two 16.3; but batch 4 over 2000 rows
 // 23.7 with one, 12.6 with the rule's.
-PagedPlan plan_paged(const Shape &s, int n_rows) {
+// For trees, bf16. Tiles of 256 columns where the rows are more than the caches hold, as each tile reads them, and hardly any column is there for nothing:
+// us, 128 / 256 columns: 60 tokens, batch 4, 32768 rows, 512 MiB 192 / 172, 8192 rows 57.7 / 54.7, 500 tokens, batch 2, 32771 rows 573 / 538, 8195 rows
+// 161 / 156, 4099 rows, 32 MiB 94.4 / 94.5, 2099 rows 61.2 / 64.4, but 328 columns (384 / 512), 9312 rows 47.5 / 50.0. Otherwise tiles of 128 by two groups
+// of four waves, where that leaves about as many waves busy as workgroups of four would be: 150 tiles on 256 CUs, batch 3, 9068 rows 73 in 450 workgroups of
+// four waves, 108 in 150 of eight; and not for the few stages of short lists, 180 rows 13.9 / 14.4.
+constexpr int64_t kRowsInCaches = 48 << 20;
+PagedPlan plan_paged(const Shape &s, int n_rows, bool tree) {
   PagedPlan p;
   const bool bf16 = s.esize == 2;
   const int64_t units = (int64_t)s.Bz * s.Hkv, cols = (int64_t)s.G * s.T;
   p.by_rows = cols <= (bf16 ? kMostRowsCols : kMostRowsColsF32);
-  const int waves = units * ((cols + 255) / 256) >= kComputeUnits ? 8 : 4;
+  const int64_t narrow = (cols + 127) / 128 * 128, wide = (cols + 255) / 256 * 256;  // columns that the products are made for
+  const bool far = tree && bf16 && wide * 20 <= narrow * 21 && units * n_rows * s.d * 2 * s.esize > kRowsInCaches;
+  const int waves = units * ((cols + 255) / 256) >= kComputeUnits || far ? 8 : 4;
   p.tile_cols = p.by_rows ? kRowsCols : waves * 32;
   p.stage_rows = p.by_rows ? 32 : kStageRows;
   p.col_tiles = (int)((cols + p.tile_cols - 1) / p.tile_cols);
@@ -98,6 +112,9 @@ PagedPlan plan_paged(const Shape &s, int n_rows) {
   if (chunks > most) chunks = most;
   if (chunks > kMostChunks) chunks = kMostChunks;
   if (chunks < 1) chunks = 1;
+  const int64_t pairs = std::min<int64_t>(kComputeUnits / tiles, most);
+  p.halves = tree && bf16 && !p.by_rows && waves == 4 && pairs > 0 && 11 * pairs >= 5 * chunks && n_rows > 4 * kStageRows;
+  if (p.halves) chunks = pairs;
   p.n_chunks = (int)chunks;
   p.workgroups = tiles * chunks;
   p.joined = p.by_rows && cols <= kMostJoinedCols && cols * chunks <= kMostJoined;

@@ -80,21 +80,26 @@ __device__ __forceinline__ void whole_step(const char *k_image, const char *v_im
 // Waves of a tile's kernel that a SIMD holds, for its __launch_bounds__.
 constexpr int tile_occupancy(int dt, int d, int waves) { return waves == 4 && dt == CKV_F32 && d == 128 ? 1 : 2; }
 
-// Args: PagedArgs, or TreeArgs, whose tokens see of the new ones what their words say.
-template <int DT, int DH, int WAVES, class Args>
+// Args: PagedArgs, or TreeArgs, whose tokens see of the new ones what their words say. GROUPS = 2: half of the
+// waves take the first half of the chunk's stages, the others the second half, for the same columns, each with buffers of its own, and they are joined
+// in LDS: as many waves as two workgroups, whose sums would go through memory and a launch. us, bf16, two workgroups / groups: 500 tokens, 32/8 heads,
+// batch 2, 4099 rows 94 / 84, 563 rows 39 / 27, 59 tokens, heads of 64, batch 12, 793 rows 24.6 / 19.0, 41 tokens, 16/2 heads, batch 8, 9312 rows 47.6 / 45.4.
+template <int DT, int DH, int WAVES, int GROUPS, class Args>
 __device__ __forceinline__ void attend_tile(const Args &a) {
   constexpr bool TREE = std::is_same<Args, TreeArgs>::value;
   typedef Image<DT, DH> I;
   constexpr int BYTES = kStageRows * I::ROW;
-  constexpr int LOADS = BYTES / 1024 / WAVES;       // of K per wave and stage, and of V
-  static_assert(LOADS * WAVES * 1024 == BYTES && kStageRows == kWave, "whole loads, a lane for every row");
-  __shared__ __align__(1024) char s_k[2][BYTES];
-  __shared__ __align__(1024) char s_v[2][BYTES];
-  __shared__ __align__(256) int32_t s_ids[2][kWave];
+  constexpr int MEMBERS = WAVES / GROUPS;           // waves of a group
+  constexpr int LOADS = BYTES / 1024 / MEMBERS;     // of K per wave and stage, and of V
+  static_assert(LOADS * MEMBERS * 1024 == BYTES && kStageRows == kWave, "whole loads, a lane for every row");
+  __shared__ __align__(1024) char s_all_k[GROUPS][2][BYTES];
+  __shared__ __align__(1024) char s_all_v[GROUPS][2][BYTES];
+  __shared__ __align__(256) int32_t s_all_ids[GROUPS][2][kWave];
   struct Offsets {
     int64_t k, v;
   };
-  __shared__ Offsets s_at[4][kStageRows];
+  __shared__ Offsets s_all_at[GROUPS][4][kStageRows];
+  __shared__ float2 s_stats[GROUPS > 1 ? MEMBERS : 1][32];
   __shared__ int s_missing, s_undefined;
   __shared__ __align__(256) uint32_t s_sees[TREE ? WAVES : 1][2][TREE ? 2 * kWave : 1];
 
@@ -103,12 +108,23 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
   const int unit = blockIdx.x % units, chunk = blockIdx.x / units % a.n_chunks;
   const int tile = a.col_tiles - 1 - blockIdx.x / units / a.n_chunks;
   const int b = unit / a.Hkv, g = unit % a.Hkv;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave_in_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const int group = GROUPS == 1 ? 0 : wave_in_all / MEMBERS, wave = GROUPS == 1 ? wave_in_all : wave_in_all % MEMBERS;
+  auto &s_k = s_all_k[group];
+  auto &s_v = s_all_v[group];
+  auto &s_ids = s_all_ids[group];
+  auto &s_at = s_all_at[group];
   const TileRange range = tile_range(a, unit, tile);
   if (range.cols <= 0) return;
-  const int first = chunk * range.per_chunk, last = min(first + range.per_chunk, range.stages);
+  int first = chunk * range.per_chunk, last = min(first + range.per_chunk, range.stages);
   const bool single = a.n_chunks == 1;
   if (first >= last && !single) return;  // the merge reads the chunks that have stages
+  const int most = GROUPS == 1 ? last - first : (last - first + 1) / 2;  // stages of the first group, which the second has too or one less
+  if (GROUPS > 1) {
+    const int between = first + most;
+    if (group == 0) last = between;
+    else first = between;
+  }
 
   const int local = wave * 32 + (lane & 31);
   const bool valid = local < range.cols;
@@ -131,10 +147,10 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
   // need them. Rows behind the end are the last one again; a page that is not in the pool is page 0 (they weigh nothing).
   auto row_of = [&](int stage) CKV_INLINE { return min(stage * kStageRows + lane, range.end - 1); };
   auto fetch_ids = [&](int stage) CKV_INLINE {
-    if (wave == stage % WAVES) dma_4(list + (row_of(stage) >> a.lists.shift), s_ids[stage & 1]);
+    if (wave == stage % MEMBERS) dma_4(list + (row_of(stage) >> a.lists.shift), s_ids[stage & 1]);
   };
   auto find_rows = [&](int stage) CKV_INLINE {
-    if (wave != stage % WAVES) return;
+    if (wave != stage % MEMBERS) return;
     const int id = s_ids[stage & 1][lane], row = row_of(stage) & ((1 << a.lists.shift) - 1);
     const bool ok = (unsigned)id < (unsigned)a.lists.n_pages;
     const int64_t page = ok ? id : 0;
@@ -163,8 +179,8 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
       const int w = (stage * kStageRows - 32 - start) >> 5;
       if (w + 2 < 0 || w >= a.words) return;  // the same for all lanes
       const uint32_t *own = words_of(a, unit) + (size_t)c.token * a.words;
-      dma_4(own + min(max(w + half, 0), a.words - 1), s_sees[wave][stage & 1]);
-      dma_4(own + min(w + 2, a.words - 1), s_sees[wave][stage & 1] + kWave);
+      dma_4(own + min(max(w + half, 0), a.words - 1), s_sees[wave_in_all][stage & 1]);
+      dma_4(own + min(w + 2, a.words - 1), s_sees[wave_in_all][stage & 1] + kWave);
     }
   };
 
@@ -193,7 +209,7 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
     if constexpr (TREE) {
       const auto word = [&](int w) CKV_INLINE {
         if (stage < 0) return words_of(a, unit)[(size_t)c.token * a.words + w];
-        return s_sees[wave][stage & 1][(w - ((stage * kStageRows - 32 - start) >> 5)) * 32 + (lane & 31)];
+        return s_sees[wave_in_all][stage & 1][(w - ((stage * kStageRows - 32 - start) >> 5)) * 32 + (lane & 31)];
       };
       const uint32_t seen = rows_of_tree(a, c.limit, z_row, z_row - start, word) >> (4 * half);
 #pragma unroll
@@ -281,6 +297,8 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
     second_product<DT, DH, false>(v + HALF, lane, weights, acc, kFinite);
     for (stage = own_last + 1; stage <= last; ++stage) advance(stage);  // the other waves' rows, and all barriers
   }
+  if (GROUPS > 1 && last - first < most)
+    for (int i = last > first ? 1 : 4; i > 0; --i) __syncthreads();  // of a stage; of the one stage and what is around it
   if (valid && not_finite(acc)) s_undefined = 1;
   __syncthreads();
   if (s_undefined) {  // the same for all waves, as there are barriers in the sweeps; one block after the other
@@ -290,16 +308,18 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
     for (int mode = kUp; mode <= kFinite; ++mode) {
       begin();
 #pragma unroll 1
-      for (int stage = first; stage < last; ++stage) {
+      for (int stage = first; stage < first + most; ++stage) {
+        const bool mine = GROUPS == 1 || stage < last;
         __syncthreads();  // the buffers have been read
-        fetch_ids(stage);
+        if (mine) fetch_ids(stage);
         wait_vm_at_most<0>();
-        find_rows(stage);
+        if (mine) find_rows(stage);
         __syncthreads();
-        fetch_k(stage);
-        fetch_v(stage);
+        if (mine) fetch_k(stage);
+        if (mine) fetch_v(stage);
         wait_vm_at_most<0>();
         __syncthreads();
+        if (!mine) continue;
 #pragma unroll 1
         for (int k = 0; k < 2; ++k) {
           f32x16_p z;
@@ -314,11 +334,45 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
     }
   }
   run.sum = over_halves(run.sum, [](float x, float y) { return x + y; });
+  if constexpr (GROUPS > 1) {
+    static_assert(GROUPS == 1 || (MEMBERS == 4 && I::DTILES * 4 * 1024 == BYTES), "a wave's sums take the place of a buffer");
+    // The second group's sums, in its rows' places, joined with the first one's as chunks are.
+    __syncthreads();
+    char *sums = wave < 2 ? s_all_k[1][wave] : s_all_v[1][wave - 2];
+    const auto place = [&](int t, int r) CKV_INLINE { return reinterpret_cast<f32x4_p *>(sums + (4 * t + r) * 1024 + lane * 16); };
+    const float inv = inverse_sum(run.sum);
+    if (group == 1) {
+#pragma unroll
+      for (int t = 0; t < I::DTILES; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) *place(t, r) = f32x4_p{acc[t][4 * r], acc[t][4 * r + 1], acc[t][4 * r + 2], acc[t][4 * r + 3]} * inv;
+      if (half == 0) s_stats[wave][lane] = make_float2(run.top, run.sum);
+    }
+    __syncthreads();
+    if (group == 1) return;
+    const float2 other = s_stats[wave][lane & 31];
+    const float top = fmaxf(run.top, other.x), ref = top == -INFINITY ? 0.0f : top;
+    float mine = run.sum * __builtin_amdgcn_exp2f(run.top - ref), its = other.y * __builtin_amdgcn_exp2f(other.x - ref);
+    const float sum = mine + its, share = inverse_sum(sum);
+    mine *= share;
+    its *= share;
+#pragma unroll
+    for (int t = 0; t < I::DTILES; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const f32x4_p own = f32x4_p{acc[t][4 * r], acc[t][4 * r + 1], acc[t][4 * r + 2], acc[t][4 * r + 3]} * inv;
+        const f32x4_p x = add_part(add_part(f32x4_p{0.0f, 0.0f, 0.0f, 0.0f}, own, mine), *place(t, r), its);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[t][4 * r + e] = x[e];
+      }
+    run.top = top;
+    run.sum = sum;
+  }
   if (!valid) return;
 
   const size_t row = (((size_t)unit * a.col_tiles + tile) * a.n_chunks + chunk) * a.tile_cols + local;
   char *to = out_row(a, b, c);
-  const float inv = inverse_sum(run.sum);
+  const float inv = GROUPS > 1 ? 1.0f : inverse_sum(run.sum);
 #pragma unroll
   for (int t = 0; t < I::DTILES; ++t)
 #pragma unroll

@@ -10,9 +10,9 @@ template <int DT, int DH, int WAVES, bool STREAM>
 __global__ void __launch_bounds__(WAVES *kWave, WAVES / 4) tree_rows_kernel(TreeArgs a) {
   attend_rows<DT, DH, WAVES, STREAM>(a);
 }
-template <int DT, int DH, int WAVES>
+template <int DT, int DH, int WAVES, int GROUPS>
 __global__ void __launch_bounds__(WAVES *kWave, tile_occupancy(DT, DH, WAVES)) tree_tile_kernel(TreeArgs a) {
-  attend_tile<DT, DH, WAVES>(a);
+  attend_tile<DT, DH, WAVES, GROUPS>(a);
 }
 
 template <int DT, int DH, int WAVES>
@@ -20,13 +20,14 @@ static void launch_rows_tree(const TreeArgs &a, hipStream_t stream) {
   if (a.col_tiles == 1) hipLaunchKernelGGL((tree_rows_kernel<DT, DH, WAVES, true>), dim3((unsigned)a.workgroups), dim3(WAVES * kWave), 0, stream, a);
   else hipLaunchKernelGGL((tree_rows_kernel<DT, DH, WAVES, false>), dim3((unsigned)a.workgroups), dim3(WAVES * kWave), 0, stream, a);
 }
-template <int DT, int DH, int WAVES>
+template <int DT, int DH, int WAVES, int GROUPS = 1>
 static void launch_tile_tree(const TreeArgs &a, hipStream_t stream) {
-  hipLaunchKernelGGL((tree_tile_kernel<DT, DH, WAVES>), dim3((unsigned)a.workgroups), dim3(WAVES * kWave), 0, stream, a);
+  hipLaunchKernelGGL((tree_tile_kernel<DT, DH, WAVES, GROUPS>), dim3((unsigned)a.workgroups), dim3(WAVES * kWave), 0, stream, a);
 }
 template <int DT, int DH>
 static void launch_tree_of(const TreeArgs &a, const PagedPlan &plan, hipStream_t stream) {
   if (plan.by_rows) launch_rows_tree<DT, DH, rows_waves(DT, DH)>(a, stream);
+  else if (plan.halves) launch_tile_tree<CKV_BF16, DH, 8, 2>(a, stream);
   else if (plan.tile_cols == 256) launch_tile_tree<DT, DH, 8>(a, stream);
   else launch_tile_tree<DT, DH, 4>(a, stream);
 }

@@ -47,11 +47,12 @@ struct PagedPlan {
   int stage_rows;    // rows of a list are shared out in multiples of this
   int n_chunks;      // workgroups along the rows of a list
   bool joined;       // chunks are joined in the same launch
+  bool halves;       // tiles of eight waves for 128 columns, of which four take one half of the rows each
   int64_t workgroups;
   size_t workspace_bytes;
 };
 constexpr int64_t kMostPagedWorkgroups = 1 << 22;  // 512 threads of each have to be fewer than 2^32
-PagedPlan plan_paged(const Shape &s, int n_rows);
+PagedPlan plan_paged(const Shape &s, int n_rows, bool tree);
 hipError_t launch_paged_attention(const ckv_params *p, const Shape &s, const PagedPlan &plan, const ckv_pages *pages, const void *q,
                                   const void *k_pages, const void *v_pages, const int32_t *table, const int32_t *length,
                                   const int32_t *count, int n_rows, const uint64_t *sees, void *out, const int64_t *out_stride, float *lse,

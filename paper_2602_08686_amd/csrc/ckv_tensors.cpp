@@ -84,12 +84,18 @@ class Tensors {
     if (!ok) refuse(name, at::kInt, {l->batch, l->n_kv_heads, l->max_pages}, "(or without the heads' axis) with the strides that the lists describe");
   }
   // Numbers of rows that stay, one list for all heads of a sequence or one for each: any strides over the axes in front of the last.
-  void add_idx(PyObject *o, const ckv_params *p) {
-    const at::Tensor *t = tensor(o, "idx");
-    if (!t) return;
+  const at::Tensor &add_idx(PyObject *o, const ckv_params *p) {
+    const at::Tensor *t = needed(o, "idx");
     bool ok = t->scalar_type() == at::kInt && (t->dim() == 2 || t->dim() == 3) && t->size(0) == p->batch && t->size(-1) > 0;
     ok = ok && (t->size(-1) == 1 || t->stride(-1) == 1) && (t->dim() == 2 || t->size(1) == p->n_kv_heads);
     if (!ok) refuse("idx", at::kInt, {p->batch, p->n_kv_heads, t->dim() > 0 ? t->size(-1) : 0}, "(or without the heads' axis) with a contiguous last axis");
+    return *t;
+  }
+  // Of a tensor's own sizes, as many axes as `dims`; added by add() with them.
+  static const at::Tensor &sized(PyObject *o, const char *name, int64_t dims) {
+    if (!THPVariable_Check(o) || THPVariable_Unpack(o).dim() != dims)
+      throw std::invalid_argument(std::string(name) + " has to be a tensor of " + std::to_string(dims) + " axes");
+    return THPVariable_Unpack(o);
   }
   // Bytes, of any type.
   Py_ssize_t add_bytes(PyObject *o, const char *name) {
@@ -119,6 +125,11 @@ class Tensors {
   }
 
  private:
+  const at::Tensor *needed(PyObject *o, const char *name) {
+    const at::Tensor *t = tensor(o, name);
+    if (!t) throw std::invalid_argument(std::string(name) + " has to be a tensor");
+    return t;
+  }
   const at::Tensor *tensor(PyObject *o, const char *name) {
     const at::Tensor *t = nullptr;
     if (o != Py_None) {
@@ -245,29 +256,43 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-int64_t number(PyObject *o) {
-  const int64_t x = PyLong_AsLongLong(o);
-  if (x == -1 && PyErr_Occurred()) {
-    PyErr_Clear();
-    throw std::invalid_argument("a size is needed");
+// The entries of `made` with `more` in front of entry `at`; both references are taken over.
+PyObject *with(PyObject *made, Py_ssize_t at, std::initializer_list<PyObject *> more) {
+  const Py_ssize_t n = made ? PyTuple_GET_SIZE(made) : 0;
+  PyObject *out = made ? PyTuple_New(n + (Py_ssize_t)more.size()) : nullptr;
+  Py_ssize_t to = 0;
+  for (Py_ssize_t i = 0; i <= n; ++i) {
+    if (i == at)
+      for (PyObject *x : more) {
+        if (out) PyTuple_SET_ITEM(out, to++, x);
+        else Py_XDECREF(x);
+      }
+    if (out && i < n) {
+      PyObject *x = PyTuple_GET_ITEM(made, i);
+      Py_INCREF(x);
+      PyTuple_SET_ITEM(out, to++, x);
+    }
   }
-  return x;
+  Py_XDECREF(made);
+  return out;
 }
 
-// (device, batch, n, parent, start, sees, positions)
+// (device, parent, start, sees, positions); in front of the addresses batch and tokens
 PyObject *tree_sees(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  return checked(n, 7, [&] {
-    const int64_t batch = number(a[1]), tokens = number(a[2]);
+  return checked(n, 5, [&] {
+    const at::Tensor &parent = Tensors::sized(a[1], "parent", 2);
+    const int64_t batch = parent.size(0), tokens = parent.size(1);
     Tensors t(a[0]);
-    t.add(a[3], "parent", at::kInt, {batch, tokens});
-    t.add(a[4], "start", at::kInt, {batch});
-    t.add(a[5], "sees", at::kLong, {batch, tokens, (tokens + 63) / 64});
-    t.add(a[6], "positions", at::kInt, {batch, tokens});
-    return t.addresses();
+    t.add(a[1], "parent", at::kInt, {batch, tokens});
+    t.add(a[2], "start", at::kInt, {batch});
+    t.add(a[3], "sees", at::kLong, {batch, tokens, (tokens + 63) / 64});
+    t.add(a[4], "positions", at::kInt, {batch, tokens});
+    PyObject *at = t.addresses();
+    return with(at, 0, {PyLong_FromLongLong(batch), PyLong_FromLongLong(tokens)});
   });
 }
 
-// (params, pages, device, table, length, count, idx, kept, k_pages, v_pages, length_out)
+// (params, pages, device, table, length, count, idx, kept, k_pages, v_pages, length_out); behind the address of idx its strides and length
 PyObject *paged_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return checked(n, 11, [&] {
     const Struct<ckv_params> p(a[0]);
@@ -278,24 +303,28 @@ PyObject *paged_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
     t.add_table(a[3], p.get(), g.get());
     t.add(a[4], "length", at::kInt, {p->batch, p->n_kv_heads});
     t.add(a[5], "count", at::kInt, {p->batch, p->n_kv_heads});
-    t.add_idx(a[6], p.get());
+    const at::Tensor &idx = t.add_idx(a[6], p.get());
     t.add(a[7], "kept", at::kInt, {p->batch, p->n_kv_heads});
     add_pools(t, p.get(), g.get(), a[8], a[9]);
     t.add(a[10], "length_out", at::kInt, {p->batch, p->n_kv_heads});
-    return t.addresses();
+    const int64_t strides[2] = {idx.stride(0), idx.dim() == 3 ? idx.stride(1) : 0};
+    PyObject *at = t.addresses();
+    return with(at, 4, {PyBytes_FromStringAndSize(reinterpret_cast<const char *>(strides), sizeof strides), PyLong_FromLongLong(idx.size(-1))});
   });
 }
 
-// (params, pages, device, n, copy, k_pages, v_pages)
+// (params, pages, device, copy, k_pages, v_pages); behind the address of copy the number of pairs
 PyObject *pages_copy(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  return checked(n, 7, [&] {
+  return checked(n, 6, [&] {
     const Struct<ckv_params> p(a[0]);
     const Struct<ckv_pages> g(a[1]);
     row_type(p.get());
+    const int64_t pairs = Tensors::sized(a[3], "copy", 2).size(0);
     Tensors t(a[2]);
-    t.add(a[4], "copy", at::kInt, {number(a[3]), 2});
-    add_pools(t, p.get(), g.get(), a[5], a[6]);
-    return t.addresses();
+    t.add(a[3], "copy", at::kInt, {pairs, 2});
+    add_pools(t, p.get(), g.get(), a[4], a[5]);
+    PyObject *at = t.addresses();
+    return with(at, 1, {PyLong_FromLongLong(pairs)});
   });
 }
 
@@ -325,19 +354,21 @@ PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// (lists, device, n_copy, table, first, end, refs, taken, copy, result)
+// (lists, device, table, first, end, refs, taken, copy, result); behind the address of copy the number of its pairs
 PyObject *pages_reserve(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  return checked(n, 10, [&] {
+  return checked(n, 9, [&] {
     const Struct<ckv_lists> held(a[0]);
     const ckv_lists *l = needed(held);
+    const int64_t pairs = a[7] == Py_None ? 0 : Tensors::sized(a[7], "copy", 2).size(0);
     Tensors t(a[1]);
-    t.add_list(a[3], "table", l);
-    t.add(a[4], "first", at::kInt, {l->batch, l->n_kv_heads});
-    t.add(a[5], "end", at::kInt, {l->batch, l->n_kv_heads});
-    add_counts(t, l, a[6], a[7]);
-    t.add(a[8], "copy", at::kInt, {number(a[2]), 2});
-    t.add(a[9], "result", at::kInt, {2});
-    return t.addresses();
+    t.add_list(a[2], "table", l);
+    t.add(a[3], "first", at::kInt, {l->batch, l->n_kv_heads});
+    t.add(a[4], "end", at::kInt, {l->batch, l->n_kv_heads});
+    add_counts(t, l, a[5], a[6]);
+    t.add(a[7], "copy", at::kInt, {pairs, 2});
+    t.add(a[8], "result", at::kInt, {2});
+    PyObject *at = t.addresses();
+    return with(at, 6, {PyLong_FromLongLong(pairs)});
   });
 }
 

@@ -91,14 +91,20 @@ def test_attention_of_trees(i):
 
 @pytest.mark.parametrize("i", [2, 5, 12, 19])
 def test_a_chain_is_the_causal_order(i):
+    """Few columns (the first and the third case): the same kernel but for the mask, and the same bits. Many: the calls share the rows out differently,
+    so that the same terms are added in another order; both are held to 64 bits, with tolerances that hold for any order of the sums."""
     c = v.TREES[i]
-    t = tree_on_gpu(dict(c, sees=v.paths(v.parents("chain", c["batch"], c["n"]))[0]), u.make(c))
+    c = dict(c, sees=v.paths(v.parents("chain", c["batch"], c["n"]))[0])
+    s = u.make(c)
+    t = tree_on_gpu(c, s)
     out, lse = attend(c, t)
     causal, also = nines(c, c["Hq"]), torch.full_like(lse, 9.0)
     B.ckv_paged_attention(t["params"], t["pages"], t["q"], t["k_pages"], t["v_pages"], t["table"], t["length"], t["n_rows"], causal, also, t["ws"],
                           count=t["count"])
     torch.cuda.synchronize()
-    assert torch.equal(out, causal) and torch.equal(lse, also)
+    check(c, s, out, lse)
+    check(c, s, causal, also)
+    assert i in (5, 19) or torch.equal(out, causal) and torch.equal(lse, also)
 
 
 @pytest.mark.parametrize("kind", ["bad_pages", "nan", "infinity"])

@@ -1,0 +1,86 @@
+"""The binding of the calls on trees, rows, pages and lists refuses tensors whose type, shape or layout is not the call's, before their addresses go
+anywhere: on the host CPU, where what is in order is refused last, for not being on a GPU."""
+import pytest
+import torch
+
+from paper_2602_08686_amd import binding as B
+
+I32, BF16 = torch.int32, torch.bfloat16
+
+
+def _tensors():
+    z = lambda *s, t=I32: torch.zeros(*s, dtype=t)  # noqa: E731
+    return dict(parent=z(2, 70), start=z(2), sees=z(2, 70, 2, t=torch.int64), positions=z(2, 70), q=z(2, 8, 70, 128, t=BF16), k_pages=z(9, 4, 16, 128, t=BF16),
+                v_pages=z(9, 4, 16, 128, t=BF16), table=z(2, 6), length=z(2, 4), count=z(2, 4), out=z(2, 8, 70, 128, t=BF16), lse=z(2, 8, 70, t=torch.float32),
+                workspace=z(1 << 20, t=torch.uint8), idx=z(2, 4, 10), kept=z(2, 4), length_out=z(2, 4), copy=z(5, 2), parents=z(2), table_out=z(2, 6), refs=z(9),
+                taken=z(1), first=z(2, 4), end=z(2, 4), result=z(2), keep=z(2, 4))
+
+
+def _calls(t, by_head):
+    g = _tensors()   # what describes them is in order
+    p = B.step_params(q=g["q"], n_q_heads=8, n_kv_heads=4)
+    table = g["table"] if not by_head else torch.zeros(2, 4, 6, dtype=I32)
+    pages, lists = B.pages_for(g["k_pages"], g["v_pages"], table), B.lists_for(table, n_kv_heads=4, n_pages=9, page_rows=16)
+    return {
+        "sees": lambda: B.ckv_tree_sees(t["parent"], t["start"], t["sees"], t["positions"]),
+        "tree": lambda: B.ckv_paged_tree_attention(p, pages, t["q"], t["k_pages"], t["v_pages"], t["table"], t["length"], 90, t["sees"], t["out"], t["lse"],
+                                                   t["workspace"], count=t["count"]),
+        "compact": lambda: B.ckv_paged_compact(p, pages, t["k_pages"], t["v_pages"], t["table"], t["length"], t["idx"], t["kept"], t["length_out"],
+                                               count=t["count"]),
+        "copy": lambda: B.ckv_pages_copy(p, pages, t["k_pages"], t["v_pages"], t["copy"]),
+        "fork": lambda: B.ckv_pages_fork(lists, t["table"], t["parents"], t["table_out"], t["refs"], t["taken"], t["length"], t["length_out"]),
+        "reserve": lambda: B.ckv_pages_reserve(lists, t["table"], t["first"], t["end"], t["refs"], t["taken"], t["copy"], t["result"]),
+        "free": lambda: B.ckv_pages_free(lists, t["table"], t["keep"], t["refs"], t["taken"]),
+    }
+
+
+long, half, strided = (lambda x: x.long()), (lambda x: x[:, :1].contiguous()), (lambda x: torch.cat([x, x], -1)[..., ::2])
+wide = lambda x: x[:, :1].expand(-1, x.shape[1])  # noqa: E731
+BAD = [
+    ("parent", ("sees",), long), ("parent", ("sees",), strided), ("parent", ("sees",), lambda x: x[0]), ("parent", ("sees",), lambda x: None),
+    ("start", ("sees",), long), ("start", ("sees",), lambda x: x[:1]), ("positions", ("sees",), long), ("positions", ("sees",), lambda x: x[:, :69]),
+    ("sees", ("sees", "tree"), lambda x: x.int()), ("sees", ("sees", "tree"), half), ("sees", ("sees", "tree"), lambda x: x[:1]),
+    ("sees", ("sees", "tree"), lambda x: x.transpose(1, 2).contiguous().transpose(1, 2)), ("sees", ("sees", "tree"), lambda x: x[:1].expand(2, -1, -1)),
+    ("q", ("tree",), lambda x: x.float()), ("q", ("tree",), lambda x: x[:, :, :69]), ("out", ("tree",), lambda x: x[:, :4]), ("lse", ("tree",), lambda x: x.double()),
+    ("length", ("tree", "compact", "fork"), long), ("length", ("tree", "compact", "fork"), wide), ("count", ("tree", "compact"), half),
+    ("table", ("tree", "compact", "fork", "reserve", "free"), long), ("table", ("tree", "compact", "fork", "reserve", "free"), lambda x: x[..., :5]),
+    ("table", ("tree", "compact", "fork", "reserve", "free"), strided), ("table_out", ("fork",), long), ("table_out", ("fork",), lambda x: x[:1]),
+    ("k_pages", ("tree", "compact", "copy"), lambda x: x.float()), ("v_pages", ("tree", "compact", "copy"), lambda x: x[1:]),
+    ("k_pages", ("tree", "compact", "copy"), lambda x: x.transpose(1, 2).contiguous().transpose(1, 2)),
+    ("idx", ("compact",), long), ("idx", ("compact",), strided), ("idx", ("compact",), lambda x: x[:, :3]), ("idx", ("compact",), lambda x: x[..., :0]),
+    ("idx", ("compact",), lambda x: x[0, 0]), ("idx", ("compact",), lambda x: None), ("kept", ("compact",), long), ("kept", ("compact",), wide),
+    ("length_out", ("compact", "fork"), long), ("length_out", ("compact", "fork"), half),
+    ("copy", ("copy", "reserve"), long), ("copy", ("copy", "reserve"), lambda x: x[:, :1]), ("copy", ("copy", "reserve"), strided),
+    ("copy", ("copy", "reserve"), lambda x: x.flatten()), ("parents", ("fork",), long), ("parents", ("fork",), lambda x: x[:1]),
+    ("refs", ("fork", "reserve", "free"), long), ("refs", ("fork", "reserve", "free"), lambda x: x[:8]), ("taken", ("fork", "reserve", "free"), long),
+    ("taken", ("fork", "reserve", "free"), lambda x: x[:0]), ("first", ("reserve",), wide), ("end", ("reserve",), long), ("result", ("reserve",), lambda x: x[:1]),
+    ("keep", ("free",), wide), ("keep", ("free",), half),
+]
+
+
+@pytest.mark.parametrize("by_head", [False, True])
+@pytest.mark.parametrize("name,calls,change", BAD, ids=[f"{b[0]}{i}" for i, b in enumerate(BAD)])
+def test_what_is_not_as_described_is_refused(by_head, name, calls, change):
+    good = _tensors()
+    if by_head:
+        good.update(table=torch.zeros(2, 4, 6, dtype=I32), table_out=torch.zeros(2, 4, 6, dtype=I32))
+    bad = dict(good, **{name: change(good[name])})
+    for call in calls:
+        with pytest.raises(ValueError, match=f"^{'parent' if name == 'parents' else name} has to be (?!on the GPU)"):
+            _calls(bad, by_head)[call]()
+
+
+@pytest.mark.parametrize("by_head", [False, True])
+def test_what_is_in_order_is_refused_for_its_place_alone(by_head):
+    good = _tensors()
+    if by_head:
+        good.update(table=torch.zeros(2, 4, 6, dtype=I32), table_out=torch.zeros(2, 4, 6, dtype=I32))
+    for name, call in _calls(good, by_head).items():
+        with pytest.raises(ValueError, match="has to be on the GPU of the call's stream"):
+            call()
+    for change in (dict(positions=None, start=None), dict(count=None), dict(idx=good["idx"][:, 0]), dict(idx=good["idx"].flip(0).transpose(0, 1)[:4].transpose(0, 1)),
+                   dict(length=None, length_out=None), dict(keep=None), dict(copy=None), dict(lse=None)):
+        t = dict(good, **change)
+        for call in ([n for n in ("sees", "tree", "compact", "fork", "reserve", "free") if not ("length" in change and n in ("tree", "compact"))]):
+            with pytest.raises(ValueError, match="has to be on the GPU of the call's stream"):
+                _calls(t, by_head)[call]()
