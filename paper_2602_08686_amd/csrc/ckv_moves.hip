@@ -23,9 +23,14 @@ struct CompactArgs {
   int splits;      // workgroups of a list
 };
 
-constexpr int kRowsAhead = 4;  // of a thread
+constexpr int kRowsOfOne = 5, kRowsOfMany = 4;  // of a thread in a round, where one round does, and where more may be needed
 
-__global__ void __launch_bounds__(1024) compact_rows_kernel(CompactArgs a) {
+// LONG: more than one round may be needed, and three of them are side by side: a row's number in the list, the pages of where it is and where it goes, and the
+// row itself, each a trip to memory behind the other. us, one round after the other / side by side: 16384 of 32768 rows, 8 heads 86 / 64, 10931 of 20114,
+// 5 lists 52 / 31. (For a single round the registers of the others cost more than they bring: 544 rows, 128 lists 13.2 / 16.0.)
+template <bool LONG>
+__global__ void __launch_bounds__(1024, LONG ? 4 : 8) compact_rows_kernel(CompactArgs a) {
+  constexpr int AHEAD = LONG ? kRowsOfMany : kRowsOfOne;
   const int unit = blockIdx.x / a.splits, slice = blockIdx.x % a.splits, b = unit / a.Hkv, g = unit % a.Hkv;
   const int length = max(a.lists.length[unit], 0);
   const int count = a.lists.count ? min(max(a.lists.count[unit], 0), length) : length, first = length - count;
@@ -37,36 +42,62 @@ __global__ void __launch_bounds__(1024) compact_rows_kernel(CompactArgs a) {
   char *base = (values ? a.v + g * a.lists.vs[1] : a.k + g * a.lists.ks[1]) + (piece - (values ? a.row_pieces : 0)) * 16;
   const int32_t *list = a.lists.table + b * a.lists.table_b + g * a.lists.table_h, *idx = a.idx + b * a.idx_b + g * a.idx_h;
   const int in_page = (1 << a.lists.shift) - 1;
-  for (int r0 = 0; r0 < m; r0 += kRowsAhead * rows) {
-    int from[kRowsAhead], from_page[kRowsAhead], to_page[kRowsAhead];
-    u32x4_d x[kRowsAhead];
+  struct Pages {
+    int from, to, row;  // row: in the list, of where it is; -1: it does not move
+  };
+  auto row_of = [&](int round, int j) CKV_INLINE { return (round * AHEAD + j) * rows + mine; };
+  auto find = [&](int round, int (&from)[AHEAD]) CKV_INLINE {
 #pragma unroll
-    for (int j = 0; j < kRowsAhead; ++j) {
-      const int r = r0 + j * rows + mine;
-      from[j] = r < m ? idx[r] : -1;
-      if (from[j] < 0 || from[j] >= count || from[j] == r || first + from[j] >= a.lists.capacity || first + r >= a.lists.capacity) from[j] = -1;
+    for (int j = 0; j < AHEAD; ++j) from[j] = row_of(round, j) < m ? idx[row_of(round, j)] : -1;
+  };
+  auto turn = [&](int round, const int (&from)[AHEAD], Pages (&p)[AHEAD]) CKV_INLINE {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int to = first + row_of(round, j), row = first + from[j];
+      const bool moves = from[j] >= 0 && from[j] < count && row != to && row < a.lists.capacity && to < a.lists.capacity;
+      p[j] = Pages{-1, -1, -1};
+      if (moves) p[j] = Pages{list[row >> a.lists.shift], list[to >> a.lists.shift], row};
     }
+  };
+  auto read = [&](Pages (&p)[AHEAD], u32x4_d (&x)[AHEAD]) CKV_INLINE {
 #pragma unroll
-    for (int j = 0; j < kRowsAhead; ++j) {
-      from_page[j] = to_page[j] = -1;
-      if (from[j] >= 0) {
-        from_page[j] = list[(first + from[j]) >> a.lists.shift];
-        to_page[j] = list[(first + r0 + j * rows + mine) >> a.lists.shift];
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < kRowsAhead; ++j) {
-      if ((unsigned)from_page[j] >= (unsigned)a.lists.n_pages || (unsigned)to_page[j] >= (unsigned)a.lists.n_pages) from[j] = -1;
+    for (int j = 0; j < AHEAD; ++j) {
+      if ((unsigned)p[j].from >= (unsigned)a.lists.n_pages || (unsigned)p[j].to >= (unsigned)a.lists.n_pages) p[j].row = -1;
       x[j] = u32x4_d{0u, 0u, 0u, 0u};
-      if (from[j] >= 0) x[j] = *reinterpret_cast<const u32x4_d *>(base + from_page[j] * s_page + ((first + from[j]) & in_page) * s_row);
+      if (p[j].row >= 0) x[j] = *reinterpret_cast<const u32x4_d *>(base + p[j].from * s_page + (p[j].row & in_page) * s_row);
     }
-    wait_vm_at_most<0>();
+  };
+  int from[AHEAD];
+  Pages here[AHEAD], next[AHEAD];
+  u32x4_d x[AHEAD];
+  find(0, from);
+  turn(0, from, here);
+  if (LONG) find(1, from);
+  read(here, x);
+  if (LONG) {
+    turn(1, from, next);
+    find(2, from);
+  }
+  for (int round = 0; LONG ? round * AHEAD * rows < m : round < 1; ++round) {
+    u32x4_d ahead[AHEAD];
+    Pages then[AHEAD];
+    if (LONG) {
+      read(next, ahead);
+      turn(round + 2, from, then);
+      find(round + 3, from);
+    }
 #pragma unroll
-    for (int j = 0; j < kRowsAhead; ++j) asm volatile("" : "+v"(x[j]));  // read in front of the barrier
+    for (int j = 0; j < AHEAD; ++j) asm volatile("" : "+v"(x[j]));  // this round's rows are there; the next one's may be on their way
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kRowsAhead; ++j)
-      if (from[j] >= 0) *reinterpret_cast<u32x4_d *>(base + to_page[j] * s_page + ((first + r0 + j * rows + mine) & in_page) * s_row) = x[j];
+    for (int j = 0; j < AHEAD; ++j) {
+      if (here[j].row >= 0) *reinterpret_cast<u32x4_d *>(base + here[j].to * s_page + ((first + row_of(round, j)) & in_page) * s_row) = x[j];
+      if (LONG) {
+        x[j] = ahead[j];
+        here[j] = next[j];
+        next[j] = then[j];
+      }
+    }
   }
 }
 
@@ -85,11 +116,16 @@ hipError_t launch_compact(const Shape &s, const ckv_pages *pages, const int32_t 
   a.cap = cap;
   a.Hkv = s.Hkv;
   a.row_pieces = s.d * s.esize / 16;
-  a.splits = (int64_t)cap * 2 * a.row_pieces <= 1024 ? 1 : a.row_pieces / 4;  // parts of 128 bytes
-  a.pieces = 2 * a.row_pieces / a.splits;
+  // Short lists by a workgroup each; others in parts of 128 bytes of a row, or 64 where long lists leave most CUs idle (us, 128 / 64 bytes: 10931 of 20114
+  // rows, 5 lists 45 / 31, 16384 of 32768, 8 lists 73 / 64, 8192 of 32768, 32 lists 62.6 / 66.5).
+  a.pieces = (int64_t)cap * 2 * a.row_pieces <= 1024 ? 2 * a.row_pieces : 8;
+  if (a.pieces == 8 && cap > 1024 && (int64_t)s.Bz * s.Hkv * a.row_pieces / 4 <= kComputeUnits / 4) a.pieces = 4;
+  a.splits = 2 * a.row_pieces / a.pieces;
   int threads = 1024;
   while (threads > 64 && (int64_t)cap * a.pieces <= threads / 2) threads /= 2;
-  hipLaunchKernelGGL(compact_rows_kernel, dim3((unsigned)(s.Bz * s.Hkv * a.splits)), dim3(threads), 0, stream, a);
+  const dim3 grid((unsigned)(s.Bz * s.Hkv * a.splits));
+  if (cap > kRowsOfOne * (threads / a.pieces)) hipLaunchKernelGGL(compact_rows_kernel<true>, grid, dim3(threads), 0, stream, a);
+  else hipLaunchKernelGGL(compact_rows_kernel<false>, grid, dim3(threads), 0, stream, a);
   return hipGetLastError();
 }
 
