@@ -309,6 +309,19 @@ __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(ReserveArgs a)
       __syncthreads();
     }
   };
+  // Without shared pages, as for prompts to come, entries need a page or nothing.
+  int need = 0, leave = 0, all_need, all_leave;
+  bool any = false;
+  entries([&](int32_t *entry, int) CKV_INLINE {
+    need += entry && !in_pool(a.to, *entry);
+    any |= entry && shared(*entry);
+  });
+  if (any) s_shared = 1;
+  scan(need, all_need);
+  if (!s_shared) {
+    if (result(all_need, 0)) entries([&](int32_t *entry, int) CKV_INLINE { give(entry, -1, entry && !in_pool(a.to, *entry)); });
+    return;
+  }
   // Counts above one are those of shared pages until they are counted down; then those that entries number, negative, are. So all entries are counted
   // down here, and whoever keeps a page counts it up again.
   entries([&](int32_t *entry, int) CKV_INLINE {
@@ -324,7 +337,7 @@ __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(ReserveArgs a)
     if (!in_pool(a.to, *entry)) return 1;
     return load_across(a.to.refs + *entry) == -1 - number ? 0 : 2;
   };
-  int need = 0, leave = 0, all_need, all_leave;
+  need = 0;
   entries([&](int32_t *entry, int number) CKV_INLINE {
     const int x = need_of(entry, number);
     need += x > 0;

@@ -91,9 +91,9 @@ __device__ __forceinline__ Column column(const PagedArgs &a, int unit, int tile,
   return c;
 }
 
-// Row of the first new token. (Read once: in a sweep it would be read from memory again and again.)
+// Row of the first new token, or one that no call looks at where it is behind them all. (Read once: in a sweep it would be read from memory again and again.)
 __device__ __forceinline__ int first_new(const PagedArgs &a, int unit) {
-  return __builtin_amdgcn_readfirstlane(max(a.lists.length[unit], 0) - new_rows(a.lists, unit, a.n));
+  return __builtin_amdgcn_readfirstlane(min(max(a.lists.length[unit], 0) - new_rows(a.lists, unit, a.n), 1 << 25));
 }
 // Which of the 32 rows from z_row on a column sees (a bit each): those in front of the new ones, and of these what its token's words say (word(w) is
 // word w of them) up to itself, which is the last one below its limit. t: new token of row z_row (below 0: in front of them).
