@@ -199,14 +199,29 @@ __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(ReserveArgs a)
     return list_of(a.to, l0 + lo) + s_entry[lo] + i - s_off[lo];
   };
 
-  // The first free pages, and how many there are.
+  // The first free pages, and how many there are. They become taken a word at a time, by the thread that has found them, up to the number that is needed
+  // (a page at a time, the bits of a round, which lie side by side, are an atomic operation each).
   int64_t page = 0;        // free pages in front of it have been found
   int have = 0, used = 0;  // of s_free
+  int wanted = 0;          // pages that are not taken yet, of those that are needed
+  auto take = [&](int64_t w, uint32_t bits, int some) CKV_INLINE {  // the first `some` of the word's pages
+    if (some <= 0 || bits == 0) return;
+    uint32_t rest = bits;
+    for (int i = __popc(bits); i > some; --i) rest &= ~(0x80000000u >> __clz((int)rest));
+    __scoped_atomic_fetch_or(a.to.taken + w, rest, __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE);
+  };
+  int place = 0;  // of the thread's first page
   auto more_free = [&](uint32_t bits) CKV_INLINE {  // of the words from page / 32 on, a thread each
     const int64_t w = (page >> 5) + tid;
     int found;
-    int to = have + scan(__popc(bits), found);
-    for (; bits && to < kFreeAhead; bits &= bits - 1) s_free[to++] = (int)(w * 32 + __builtin_ctz(bits));
+    place = have + scan(__popc(bits), found);
+    int to = place;
+    for (uint32_t rest = bits; rest && to < kFreeAhead; rest &= rest - 1) s_free[to++] = (int)(w * 32 + __builtin_ctz(rest));
+    if (wanted > 0) {
+      const int upto = min(kFreeAhead, have + wanted);
+      take(w, bits, upto - place);
+      wanted -= min(found, upto - have);
+    }
     __syncthreads();
     const bool full = have + found >= kFreeAhead;
     page = full ? (int64_t)s_free[kFreeAhead - 1] + 1 : ((page >> 5) + kReserveThreads) * 32;
@@ -252,16 +267,19 @@ __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(ReserveArgs a)
       }
       *entry = now;
       store_across(a.to.refs + now, 1);
-      take_page(a.to, now);
     }
     used += asked;
     pairs += total >> 16;
   };
-  auto result = [&](int need, int leave) CKV_INLINE {  // whether there is enough
+  auto result = [&](int need, int leave) CKV_INLINE {  // whether there is enough; the pages that have been found are taken then
     const int missing = max(max(need - all_free, leave - a.n_copy), 0);
     if (tid == 0) {
       a.result[0] = missing;
       a.result[1] = missing ? 0 : leave;
+    }
+    if (missing == 0) {
+      take(tid, first_bits, min(need, kFreeAhead) - place);
+      wanted = need - min(need, have);
     }
     return missing == 0;
   };
