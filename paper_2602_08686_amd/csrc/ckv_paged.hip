@@ -112,7 +112,7 @@ PagedPlan plan_paged(const Shape &s, int n_rows, bool tree) {
   if (chunks > most) chunks = most;
   if (chunks > kMostChunks) chunks = kMostChunks;
   if (chunks < 1) chunks = 1;
-  const int64_t pairs = std::min<int64_t>(kComputeUnits / tiles, most);
+  const int64_t pairs = std::min<int64_t>({kComputeUnits / tiles, most, kMostChunks});
   p.halves = tree && bf16 && !p.by_rows && waves == 4 && pairs > 0 && 11 * pairs >= 5 * chunks && n_rows > 4 * kStageRows;
   if (p.halves) chunks = pairs;
   p.n_chunks = (int)chunks;

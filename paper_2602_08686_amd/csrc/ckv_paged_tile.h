@@ -92,6 +92,7 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
   constexpr int MEMBERS = WAVES / GROUPS;           // waves of a group
   constexpr int LOADS = BYTES / 1024 / MEMBERS;     // of K per wave and stage, and of V
   static_assert(LOADS * MEMBERS * 1024 == BYTES && kStageRows == kWave, "whole loads, a lane for every row");
+  static_assert(GROUPS == 1 || TREE, "the second group waits at as many barriers as the first, which are counted for trees");
   __shared__ __align__(1024) char s_all_k[GROUPS][2][BYTES];
   __shared__ __align__(1024) char s_all_v[GROUPS][2][BYTES];
   __shared__ __align__(256) int32_t s_all_ids[GROUPS][2][kWave];
@@ -225,11 +226,18 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
 
   begin();
   if (first < last) {
-    for (int i = 0; i < 2; ++i) {  // the first two stages' rows, each by its wave, one behind the other
-      fetch_ids(first + i);
+    if constexpr (TREE) {  // the first two stages' rows, each by its wave
+      for (int i = 0; i < 2; ++i) fetch_ids(first + i);
       wait_vm_at_most<0>();
-      find_rows(first + i);
+      for (int i = 0; i < 2; ++i) find_rows(first + i);
       __syncthreads();
+    } else {  // ... one behind the other
+      for (int i = 0; i < 2; ++i) {
+        fetch_ids(first + i);
+        wait_vm_at_most<0>();
+        find_rows(first + i);
+        __syncthreads();
+      }
     }
     fetch_ids(first + 2);
     fetch_k(first);
@@ -298,7 +306,7 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
     for (stage = own_last + 1; stage <= last; ++stage) advance(stage);  // the other waves' rows, and all barriers
   }
   if (GROUPS > 1 && last - first < most)
-    for (int i = last > first ? 1 : 4; i > 0; --i) __syncthreads();  // of a stage; of the one stage and what is around it
+    for (int i = last > first ? 1 : 3; i > 0; --i) __syncthreads();  // of a stage; of the one stage and what is around it
   if (valid && not_finite(acc)) s_undefined = 1;
   __syncthreads();
   if (s_undefined) {  // the same for all waves, as there are barriers in the sweeps; one block after the other

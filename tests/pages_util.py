@@ -133,6 +133,24 @@ TREES = [
     tree_case("chain", n=257, heads=(2, 1), lengths=((1400,), (257,)), page=16),                    # tiles, chunks along the rows
 ]
 
+# Those that reach the kernels' other instances, on the GPU: eight waves where the tiles fill the chip or the rows are more than the caches hold.
+MANY = [
+    tree_case(n=24, heads=(32, 8), lengths=((544, 300, 60, 33, 100, 544, 31, 32),) * 3, by_head=True, page=32),
+    tree_case(n=60, heads=(8, 2), lengths=((5000, 5000), (3003, 3003)), page=16),
+    tree_case("noise", n=25, heads=(7, 1), lengths=((9001,), (40,), (2000,)), counts=((25,), (13,), (25,)), page=16, pool_token_major=True),
+    tree_case("empty", n=300, heads=(4, 1), lengths=((1000,), (300,)), page=64),
+    tree_case(n=257, heads=(32, 32), lengths=tuple((257 + 100 * b,) * 32 for b in range(4)), page=16),
+    tree_case("noise", n=600, heads=(2, 1), d=64, lengths=((2000,),), counts=((590,),), page=128),
+    tree_case("noise", dtype="f32", n=300, heads=(4, 1), lengths=((1100,),), page=16),
+    tree_case("empty", dtype="f32", n=64, heads=(4, 1), lengths=((3000,), (70,)), page=8),
+    tree_case(dtype="f32", d=64, n=8, heads=(4, 2), lengths=((100, 37),), by_head=True, page=16),
+    tree_case("noise", d=64, n=20, heads=(2, 1), lengths=((333,), (21,)), page=4),
+    tree_case("noise", d=64, n=257, heads=(32, 32), lengths=tuple((257 + 60 * b,) * 32 for b in range(4)), page=32),
+    tree_case(dtype="f32", n=257, heads=(32, 32), lengths=tuple((257 + 40 * b,) * 32 for b in range(4)), page=32),
+    tree_case("empty", dtype="f32", d=64, n=257, heads=(32, 32), lengths=((257,) * 32, (300,) * 32, (20,) * 32, (257,) * 32),
+              counts=((257,) * 32, (257,) * 32, (257,) * 32, (3,) * 32), page=16),
+]
+
 
 # ---- rows that move ---------------------------------------------------------------------------------------------------------
 def chosen(c, cap, kept, each_head, seed=0):

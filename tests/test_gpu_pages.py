@@ -61,16 +61,7 @@ def check(c, s, out, lse):
     u.check(host(lse), np.where(old, 9.0, wl), lt, "lse")
 
 
-LONG = [
-    v.tree_case(n=24, heads=(32, 8), lengths=((544, 300, 60, 33, 100, 544, 31, 32),) * 3, by_head=True, page=32),
-    v.tree_case(n=60, heads=(8, 2), lengths=((5000, 5000), (3003, 3003)), page=16),
-    v.tree_case("noise", n=25, heads=(7, 1), lengths=((9001,), (40,), (2000,)), counts=((25,), (13,), (25,)), page=16, pool_token_major=True),
-    v.tree_case("empty", n=300, heads=(4, 1), lengths=((1000,), (300,)), page=64),
-    v.tree_case(n=257, heads=(32, 32), lengths=tuple((257 + 100 * b,) * 32 for b in range(4)), page=16),      # tiles of eight waves
-    v.tree_case("noise", n=600, heads=(2, 1), d=64, lengths=((2000,),), counts=((590,),), page=128),
-    v.tree_case("noise", dtype="f32", n=300, heads=(4, 1), lengths=((1100,),), page=16),
-    v.tree_case("empty", dtype="f32", n=64, heads=(4, 1), lengths=((3000,), (70,)), page=8),
-]
+LONG = v.MANY
 
 
 @pytest.mark.parametrize("i", range(len(v.TREES) + len(LONG)))
@@ -133,6 +124,35 @@ def test_what_a_token_does_not_see_has_no_influence(i, kind):
     out, lse = attend(c, t)
     torch.cuda.synchronize()
     check(c, s, out, lse)
+
+
+@pytest.mark.parametrize("n,d", [(60, 128), (2, 128), (20, 64), (80, 64)])
+def test_a_bound_far_above_the_lengths(n, d):
+    """A call that was planned for long lists (a graph, say) on short ones, down to none."""
+    for lengths, counts in ((((n + 40, n + 9),), ((n, n),)), (((1, 1),), ((1, 1),)), (((0, 0),), ((n, 0),)), (((700, 2),), ((n, 2),)), (((9000, n),), ((n, n),))):
+        c = v.tree_case("random", n=n, d=d, heads=(8, 2), lengths=lengths, counts=counts, page=16)
+        s = u.make(c)
+        s["table"] = np.concatenate([s["table"], np.full((1, 16000 - s["table"].shape[1]), -1, np.int32)], 1)
+        t = tree_on_gpu(c, s)
+        assert t["n_rows"] == 256000 and t["ws"] is not None
+        out, lse = attend(c, t)
+        torch.cuda.synchronize()
+        check(c, dict(s, table=s["table"][:, :600]), out, lse)
+
+
+def test_lengths_behind_the_bound_and_below_zero():
+    """Lists that say they are longer than the call looks, by a little and by far: none of the drafted tokens' rows is seen, or some are."""
+    c = v.tree_case("random", n=30, heads=(4, 2), lengths=((300, 280),), page=16)
+    s = u.make(c)
+    for lengths, n_rows in (((300, 280), 290), ((300, 280), 271), ((2 ** 31 - 1, 280), 280), ((-5, -2 ** 31), 300)):
+        d = dict(c, lengths=np.array([lengths], np.int32), n_rows=n_rows)
+        t = tree_on_gpu(dict(c, n_rows=n_rows), s)
+        t["length"] = ints(d["lengths"])
+        out, lse = attend(d, t)
+        torch.cuda.synchronize()
+        want = v.attention(dict(d, lengths=np.minimum(d["lengths"], 1 << 20)), s)   # (rows behind the bound are not looked at)
+        u.check(host(out), want[0], want[1], "out")
+        u.check(host(lse), want[2], want[3], "lse")
 
 
 # ---- rows and pages that move -------------------------------------------------------------------------------------------------

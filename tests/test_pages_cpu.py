@@ -2,6 +2,7 @@
 instead of a GPU: against results in 64 bits, with page numbers that are none, memory that ends at a page without access, and infinities and NaN
 where nobody looks."""
 import ctypes
+import re
 
 import numpy as np
 import pytest
@@ -126,6 +127,35 @@ def _causal(path):
 
 def test_a_chain_is_the_causal_order(lib_path):
     in_child(_causal, lib_path)
+
+
+def _all_instances(path):
+    """(kernel, its template arguments) of the launches that the tests' cases make."""
+    lib = cpu.load(path)
+    lib.emu_set_dry(1)
+    lib.emu_launched()
+    got = set()
+    at = ctypes.c_void_p(4096)   # no kernel runs: nothing is there
+    for c in v.TREES + v.MANY:
+        s = u.make(c)
+        p, n_rows = u.params(c, s), c["n_rows"] or s["table"].shape[-1] * c["page"]
+        need = lib.ckv_paged_workspace_bytes(ref(p), n_rows)
+        assert lib.ckv_paged_tree_attention(ref(p), ref(u.pages(c, s)), at, at, at, at, at, None, n_rows, at, at, None, None, at, ctypes.c_size_t(need),
+                                            None) == B.CKV_OK
+        for line in lib.emu_launched().decode().splitlines():
+            kernel, own = re.match(r"\((\w+)<(.*)>\)", line.split("|")[0]).groups()
+            where = line.split("|")[1]
+            given = dict(re.findall(r"(\w+) = (\w+)", where[where.index("["):]))
+            got.add((kernel, tuple(given.get(a, a) for a in own.replace(" ", "").split(","))))
+    types = [(t, d) for t in "01" for d in ("64", "128")]   # f32, bf16
+    want = {("tree_tile_kernel", (t, d, w, "1")) for t, d in types for w in "48"} | {("tree_tile_kernel", ("1", d, "8", "2")) for d in ("64", "128")}
+    want |= {("tree_rows_kernel", (t, d, "4" if (t, d) == ("0", "128") else "8", stream)) for t, d in types for stream in ("true", "false")}
+    want |= {("paged_merge_kernel", x) for x in types}
+    assert got == want, (sorted(want - got), sorted(got - want))
+
+
+def test_every_instance_is_reached(lib_path):
+    in_child(_all_instances, lib_path)
 
 
 # ---- rows and pages that move -------------------------------------------------------------------------------------------------
