@@ -9,6 +9,7 @@ import pytest
 
 import cpu_build as cpu
 import paged_util as u
+import paged_values as pv
 import pages_util as v
 from paper_2602_08686_amd import binding as B
 from test_cpu_build import in_child
@@ -107,6 +108,24 @@ def _tree_odd(path, c, kind):
 @pytest.mark.parametrize("i", [1, 4, 5, 8, 12, 15, 18])
 def test_what_a_token_does_not_see_has_no_influence(lib_path, i, kind):
     in_child(_tree_odd, lib_path, v.TREES[i], kind)
+
+
+def _tree_values(path, c, kind):
+    first = int(c["lengths"].min()) - c["n"]
+    if kind == "high":
+        s = pv.high(c, 0.25, 3e38, "mixed", True)
+    elif kind == "earlier":
+        s = pv.earlier(c, 5, 133, 300.0)
+    else:
+        s = pv.make(c, {first + t: (None, dict(pv.BAD) if t % 2 else {9: pv.INF}) for t in range(0, c["n"], 3)})
+    s = _fenced(s)
+    _check(c, s, *_attend(cpu.load(path), c, s))
+
+
+@pytest.mark.parametrize("kind", ["high", "earlier", "drafted"])
+@pytest.mark.parametrize("c", [pv.FEW[0], pv.FEW[3], pv.MANY[0], pv.MANY[3]], ids=range(4))
+def test_values_that_are_not_finite_or_nearly_so(lib_path, c, kind):
+    in_child(_tree_values, lib_path, dict(c, sees=v.paths(v.parents("random", c["batch"], c["n"]))[0]), kind)
 
 
 def _causal(path):
