@@ -791,7 +791,7 @@ extern "C" ckv_status ckv_paged_tree_attention(const ckv_params *params, const c
 extern "C" ckv_status ckv_tree_sees(int32_t batch, int32_t n, const int32_t *parent, const int32_t *start, uint64_t *sees, int32_t *positions,
                                     void *hip_stream) {
   if (batch < 1 || n < 1 || !parent || !sees || ((uintptr_t)sees & 7) || (positions && !start)) return CKV_EINVAL;
-  if (n > kMostDrafts || (int64_t)batch * n > INT32_MAX / 64) return CKV_EUNSUPPORTED;
+  if (n > kMostDrafts || tree_workgroups(batch, n) > kMostPagedWorkgroups) return CKV_EUNSUPPORTED;
   return launch_tree_sees(batch, n, parent, start, sees, positions, (hipStream_t)hip_stream) == hipSuccess ? CKV_OK : CKV_EHIP;
 }
 
@@ -807,7 +807,7 @@ extern "C" ckv_status ckv_paged_compact(const ckv_params *params, const ckv_page
   if (st != CKV_OK) return st;
   Shape s;
   derive(params, &s);
-  if ((int64_t)s.Bz * s.Hkv > INT32_MAX / 1024) return CKV_EUNSUPPORTED;  // workgroups of a launch
+  if ((int64_t)s.Bz * s.Hkv > kMostCompactLists) return CKV_EUNSUPPORTED;
   if (launch_compact(s, pages, table, length, count, idx, idx_stride, cap, kept, k_pages, v_pages, length_out, (hipStream_t)hip_stream) != hipSuccess)
     return CKV_EHIP;
   return CKV_OK;
@@ -835,7 +835,7 @@ static ckv_status lists_refused(const ckv_lists *l) {
   if (l->batch > 1 && l->table_stride[0] < l->max_pages) return CKV_EINVAL;
   if (l->page_rows > 65536 || (l->page_rows & (l->page_rows - 1))) return CKV_EUNSUPPORTED;
   if ((int64_t)l->page_rows * l->max_pages > INT32_MAX) return CKV_EUNSUPPORTED;
-  if ((int64_t)l->batch * l->n_kv_heads > INT32_MAX / l->max_pages) return CKV_EUNSUPPORTED;
+  if ((int64_t)l->batch * l->n_kv_heads > INT32_MAX / l->max_pages || entry_workgroups(l) > kMostPagedWorkgroups) return CKV_EUNSUPPORTED;
   return CKV_OK;
 }
 
@@ -853,6 +853,7 @@ extern "C" ckv_status ckv_pages_reserve(const ckv_lists *lists, int32_t *table, 
   const ckv_status st = lists_refused(lists);
   if (st != CKV_OK) return st;
   if (!table || !first || !end || !refs || !taken || !result || n_copy < 0 || (n_copy > 0 && !copy)) return CKV_EINVAL;
+  if (n_copy > INT32_MAX / 4) return CKV_EUNSUPPORTED;
   return launch_reserve(lists, table, first, end, refs, taken, copy, n_copy, result, (hipStream_t)hip_stream) == hipSuccess ? CKV_OK : CKV_EHIP;
 }
 

@@ -49,6 +49,8 @@ __device__ __forceinline__ void release_page(const ListArgs &a, int p) {
 __device__ __forceinline__ int32_t *list_of(const ListArgs &a, int l) { return a.table + l / a.heads * a.table_b + l % a.heads * a.table_h; }
 
 constexpr int kEntryThreads = 256;
+static int blocks_of(int max_pages) { return (max_pages - 1) / kEntryThreads + 1; }  // of a list
+int64_t entry_workgroups(const ckv_lists *l) { return (int64_t)l->batch * l->n_kv_heads * blocks_of(l->max_pages); }
 
 // ---------------------------------------------------------------------------------------------
 // Lists that become copies
@@ -89,7 +91,7 @@ hipError_t launch_fork(const ckv_lists *lists, const int32_t *table, const int32
   a.length = length;
   a.length_out = length_out;
   a.batch = lists->batch;
-  a.blocks = (lists->max_pages + kEntryThreads - 1) / kEntryThreads;
+  a.blocks = blocks_of(lists->max_pages);
   hipLaunchKernelGGL(fork_kernel, dim3((unsigned)a.to.lists * a.blocks), dim3(kEntryThreads), 0, stream, a);
   return hipGetLastError();
 }
@@ -116,7 +118,7 @@ __global__ void __launch_bounds__(kEntryThreads) free_kernel(ListArgs a, const i
 
 hipError_t launch_free(const ckv_lists *lists, int32_t *table, const int32_t *keep, int32_t *refs, uint32_t *taken, hipStream_t stream) {
   const ListArgs a = list_args(lists, table, refs, taken);
-  const int blocks = (a.max_pages + kEntryThreads - 1) / kEntryThreads;
+  const int blocks = blocks_of(a.max_pages);
   hipLaunchKernelGGL(free_kernel, dim3((unsigned)a.lists * blocks), dim3(kEntryThreads), 0, stream, a, keep, blocks);
   return hipGetLastError();
 }

@@ -34,8 +34,9 @@ __global__ void __launch_bounds__(1024, LONG ? 4 : 8) compact_rows_kernel(Compac
   const int unit = blockIdx.x / a.splits, slice = blockIdx.x % a.splits, b = unit / a.Hkv, g = unit % a.Hkv;
   const int length = max(a.lists.length[unit], 0);
   const int count = a.lists.count ? min(max(a.lists.count[unit], 0), length) : length, first = length - count;
-  const int m = min(max(a.kept[unit], 0), min(count, a.cap));
-  if (slice == 0 && threadIdx.x == 0) a.length_out[unit] = first + m;
+  const int stay = min(max(a.kept[unit], 0), min(count, a.cap));
+  if (slice == 0 && threadIdx.x == 0) a.length_out[unit] = first + stay;
+  const int m = min(stay, min(a.lists.capacity, INT32_MAX - (1 << 16)) - first);  // rows behind the list's pages go nowhere; room for the rounds ahead
   const int piece = slice * a.pieces + threadIdx.x % a.pieces, rows = blockDim.x / a.pieces, mine = threadIdx.x / a.pieces;
   const bool values = piece >= a.row_pieces;
   const int64_t s_page = values ? a.lists.vs[0] : a.lists.ks[0], s_row = values ? a.lists.vs[2] : a.lists.ks[2];

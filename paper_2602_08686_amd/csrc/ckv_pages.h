@@ -61,9 +61,11 @@ hipError_t launch_paged_attention(const ckv_params *p, const Shape &s, const Pag
 // Trees of drafted tokens.
 constexpr int kMostTreeTokens = 65536;  // a token's words times the tokens stay below 2^31
 constexpr int kMostDrafts = 4096;       // of ckv_tree_sees: a word and a number of each in LDS
+int64_t tree_workgroups(int batch, int n);
 hipError_t launch_tree_sees(int batch, int n, const int32_t *parent, const int32_t *start, uint64_t *sees, int32_t *positions, hipStream_t stream);
 
 // Rows and pages that move.
+constexpr int kMostCompactLists = 1 << 17;  // a list has 16 workgroups of 1024 threads at most, and those of a launch have to be fewer than 2^32
 hipError_t launch_compact(const Shape &s, const ckv_pages *pages, const int32_t *table, const int32_t *length, const int32_t *count,
                           const int32_t *idx, const int64_t *idx_stride, int cap, const int32_t *kept, void *k_pages, void *v_pages,
                           int32_t *length_out, hipStream_t stream);
@@ -71,6 +73,7 @@ int64_t copy_workgroups(const Shape &s, const ckv_pages *pages, int n);
 hipError_t launch_pages_copy(const Shape &s, const ckv_pages *pages, const int32_t *copy, int n, void *k_pages, void *v_pages, hipStream_t stream);
 
 // Which lists have which pages.
+int64_t entry_workgroups(const ckv_lists *lists);  // at most, of a launch with a thread for an entry
 hipError_t launch_fork(const ckv_lists *lists, const int32_t *table, const int32_t *parent, int32_t *table_out, int32_t *refs, uint32_t *taken,
                        const int32_t *length, int32_t *length_out, hipStream_t stream);
 hipError_t launch_reserve(const ckv_lists *lists, int32_t *table, const int32_t *first, const int32_t *end, int32_t *refs, uint32_t *taken,

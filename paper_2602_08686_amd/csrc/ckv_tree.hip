@@ -71,8 +71,10 @@ __global__ void __launch_bounds__(kTreeThreads) tree_sees_kernel(const int32_t *
   if (positions && i < n) positions[(size_t)b * n + i] = (int32_t)((uint32_t)from0 + (uint32_t)depth);
 }
 
+int64_t tree_workgroups(int batch, int n) { return (int64_t)batch * ((n + kTreeThreads - 1) / kTreeThreads); }
+
 hipError_t launch_tree_sees(int batch, int n, const int32_t *parent, const int32_t *start, uint64_t *sees, int32_t *positions, hipStream_t stream) {
-  const dim3 grid((unsigned)batch * ((n + kTreeThreads - 1) / kTreeThreads));
+  const dim3 grid((unsigned)tree_workgroups(batch, n));
   if (n <= 1024) hipLaunchKernelGGL(tree_sees_kernel<1024>, grid, dim3(kTreeThreads), 0, stream, parent, start, sees, positions, n);
   else hipLaunchKernelGGL(tree_sees_kernel<kMostDrafts>, grid, dim3(kTreeThreads), 0, stream, parent, start, sees, positions, n);
   return hipGetLastError();

@@ -211,6 +211,30 @@ def test_rows_that_stay_move_together(lib_path, i, bad):
     in_child(_compact, lib_path, *v.MOVES[i], bad)
 
 
+def _compact_odd(path):
+    """Lengths behind the lists' pages, by a little and by far, and below zero: rows that are on a page move, nothing else is touched."""
+    lib = cpu.load(path)
+    base = u.case(n=1, lengths=((96, 90),), page=16)
+    for lengths, counts in (((200, 97), None), ((2 ** 31 - 1, 130), None), ((120, 100), (60, 20)), ((2 ** 31 - 1, 2 ** 31 - 20), (40, 2 ** 31 - 1)), ((-3, -2 ** 31), (5, 9))):
+        c = dict(base, lengths=np.array([lengths], np.int32), counts=None if counts is None else np.array([counts], np.int32))
+        s = u.make(base)
+        idx = np.sort(np.random.default_rng(4).permutation(150)[:40]).astype(np.int32)[None]
+        kept = np.array([[40, 33]], np.int32)
+        want, length_out = v.compacted(c, s, idx, kept)
+        s, got = _fenced(s), _at_fence(np.full_like(c["lengths"], 9))
+        st = lib.ckv_paged_compact(ref(u.params(base, s)), ref(u.pages(base, s)), P(s["table"]), P(_at_fence(c["lengths"])),
+                                   P(None if counts is None else _at_fence(c["counts"])), P(_at_fence(idx)), (ctypes.c_int64 * 2)(40, 0), 40,
+                                   P(_at_fence(kept)), P(s["k_pages"]), P(s["v_pages"]), P(got), None)
+        assert st == B.CKV_OK
+        for m in ("k_pages", "v_pages"):
+            _same(s[m], want[m], m)
+        assert np.array_equal(got, length_out)
+
+
+def test_lengths_that_no_list_has(lib_path):
+    in_child(_compact_odd, lib_path)
+
+
 def _copy(path, c, pairs):
     lib, s = cpu.load(path), u.make(c)
     n = s["k_pages"].shape[0]

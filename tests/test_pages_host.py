@@ -75,7 +75,8 @@ def test_struct_layout_matches_the_header():
 def test_trees_are_refused():
     for kw in (dict(batch=0), dict(n=0), dict(parent=None), dict(sees=None), dict(start=None), dict(sees=ctypes.c_void_p(4100))):
         assert _sees(**kw) == B.CKV_EINVAL, kw
-    assert _sees(n=4097) == B.CKV_EUNSUPPORTED and _sees(batch=1 << 20, n=4096) == B.CKV_EUNSUPPORTED
+    assert _sees(n=4097) == B.CKV_EUNSUPPORTED
+    assert _sees(batch=1 << 20, n=4096) == B.CKV_EUNSUPPORTED and _sees(batch=(1 << 22) + 1, n=1) == B.CKV_EUNSUPPORTED   # a launch's workgroups
 
 
 def test_tree_attention_refuses():
@@ -104,7 +105,7 @@ def test_compact_refuses():
     assert _compact(length_out=AT) == B.CKV_EINVAL                                    # the lengths that are read
     assert _compact(stride=(ctypes.c_int64 * 2)(-1, 0)) == B.CKV_EINVAL and _compact(stride=(ctypes.c_int64 * 2)(9, -9)) == B.CKV_EINVAL
     assert _compact(p=_params(d=96)) == B.CKV_EUNSUPPORTED
-    assert _compact(p=_params(batch=1 << 20, n_q_heads=4)) == B.CKV_EUNSUPPORTED
+    assert _compact(p=_params(batch=(1 << 16) + 1, n_q_heads=4)) == B.CKV_EUNSUPPORTED   # a launch's workgroups
     assert _compact(pages=_pages(page_rows=24)) == B.CKV_EUNSUPPORTED and _compact(pages=_pages(k_stride=(2, 64))) == B.CKV_EINVAL
 
 
@@ -123,7 +124,7 @@ def test_copy_refuses():
     (dict(max_pages=0), B.CKV_EINVAL), (dict(reserved=1), B.CKV_EINVAL), (dict(table_stride=(0, -1)), B.CKV_EINVAL),
     (dict(table_stride=(1, -50)), B.CKV_EINVAL), (dict(table_stride=(1, 49)), B.CKV_EINVAL), (dict(table_stride=(0, 49)), B.CKV_EINVAL),
     (dict(page_rows=24), B.CKV_EUNSUPPORTED), (dict(page_rows=1 << 17), B.CKV_EUNSUPPORTED), (dict(max_pages=1 << 28, table_stride=(1, 0)), B.CKV_EINVAL),
-    (dict(batch=1 << 28), B.CKV_EUNSUPPORTED),
+    (dict(batch=1 << 28), B.CKV_EUNSUPPORTED), (dict(batch=(1 << 21) + 1, max_pages=1), B.CKV_EUNSUPPORTED),
 ])
 def test_lists_are_refused(bad, status):
     l = _lists(**bad)
@@ -138,7 +139,7 @@ def test_calls_on_lists_refuse():
     assert _fork(l, out=AT) == B.CKV_EINVAL and _fork(l, length_out=AT) == B.CKV_EINVAL  # in place
     for name in ("table", "first", "end", "refs", "taken", "copy", "result"):
         assert _reserve(l, **{name: None}) == B.CKV_EINVAL, name
-    assert _reserve(l, n=-1) == B.CKV_EINVAL
+    assert _reserve(l, n=-1) == B.CKV_EINVAL and _reserve(l, n=1 << 30) == B.CKV_EUNSUPPORTED
     for name in ("table", "refs", "taken"):
         assert _free(l, **{name: None}) == B.CKV_EINVAL, name
 
