@@ -99,6 +99,7 @@ hipError_t launch_fork(const ckv_lists *lists, const int32_t *table, const int32
 // ---------------------------------------------------------------------------------------------
 // Pages that are given back
 // ---------------------------------------------------------------------------------------------
+// A thread for an entry: a launch (64 lists of 563 entries 3.4 us; 32 of 2048, all pages released, 5.4 among a graph's kernels).
 __global__ void __launch_bounds__(kEntryThreads) free_kernel(ListArgs a, const int32_t *keep, int blocks) {
   const int l = blockIdx.x / blocks, e = blockIdx.x % blocks * kEntryThreads + threadIdx.x;
   int rows = 0;

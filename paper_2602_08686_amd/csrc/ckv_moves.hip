@@ -10,7 +10,9 @@ namespace ckv {
 // In place: row r of the moved ones comes from idx[r] >= r (ascending numbers, none twice), so what is written for r holds no source of a later
 // row, and the sources that it does hold are those of rows up to r. Reads may run ahead of writes as far as they like; a write waits for the
 // reads of its own round and the earlier ones, which a workgroup that takes a list's rows in order has behind a barrier a round. The pieces of a row are
-// independent, so keys, values and parts of rows go to workgroups of their own.
+// independent, so keys, values and parts of rows go to workgroups of their own. Short lists are a chain of four trips to memory (lengths, numbers, pages, rows):
+// seven accepted rows of 16 sequences, 8 heads 3.6 us, up to 544 kept rows of 32 lists 6.7; long ones are bound by what a few workgroups a list have in
+// flight (bf16, 8 lists, 16384 of 32768 rows 64 us, 2.1 TB/s) or by memory (f32, 48 lists, 9362 of 14438 rows 170 us, 4 TB/s of rows read and written).
 struct CompactArgs {
   PageLists lists;  // count null: all rows of a list
   char *k, *v;
@@ -133,6 +135,8 @@ hipError_t launch_compact(const Shape &s, const ckv_pages *pages, const int32_t 
 // ---------------------------------------------------------------------------------------------
 // Pages
 // ---------------------------------------------------------------------------------------------
+// A workgroup takes 32 KiB of a pair, a thread eight pieces of 16 bytes, all read before the first is written. Memory bound: bf16, 1000 pages of 64 rows of 8 heads
+// 106.5 us, 4.9 TB/s read and written (a plain copy of a gigabyte 5.1); 16 pages of 16 rows 3.3 us, a launch.
 struct CopyArgs {
   char *k, *v;
   const int32_t *copy;
