@@ -790,7 +790,7 @@ extern "C" ckv_status ckv_paged_tree_attention(const ckv_params *params, const c
 
 extern "C" ckv_status ckv_tree_sees(int32_t batch, int32_t n, const int32_t *parent, const int32_t *start, uint64_t *sees, int32_t *positions,
                                     void *hip_stream) {
-  if (batch < 1 || n < 1 || !parent || !sees || ((uintptr_t)sees & 7) || (positions && !start)) return CKV_EINVAL;
+  if (batch < 1 || n < 1 || !parent || !sees || ((uintptr_t)sees & 7) || (positions && !start) || positions == parent) return CKV_EINVAL;
   if (n > kMostDrafts || tree_workgroups(batch, n) > kMostPagedWorkgroups) return CKV_EUNSUPPORTED;
   return launch_tree_sees(batch, n, parent, start, sees, positions, (hipStream_t)hip_stream) == hipSuccess ? CKV_OK : CKV_EHIP;
 }
@@ -800,7 +800,8 @@ extern "C" ckv_status ckv_paged_compact(const ckv_params *params, const ckv_page
                                         void *k_pages, void *v_pages, int32_t *length_out, void *hip_stream) {
   ckv_status st = validate(params);
   if (st != CKV_OK) return st;
-  if (!table || !length || !idx || !kept || !k_pages || !v_pages || !length_out || length_out == length || cap < 1) return CKV_EINVAL;
+  if (!table || !length || !idx || !kept || !k_pages || !v_pages || !length_out || cap < 1) return CKV_EINVAL;
+  if (length_out == length || length_out == count || length_out == kept) return CKV_EINVAL;  // a list's workgroups read these, one of them writes
   if (misaligned({k_pages, v_pages})) return CKV_EINVAL;
   if (idx_stride && (idx_stride[0] < 0 || idx_stride[1] < 0)) return CKV_EINVAL;
   st = pages_refused(params, pages);
@@ -844,7 +845,7 @@ extern "C" ckv_status ckv_pages_fork(const ckv_lists *lists, const int32_t *tabl
   const ckv_status st = lists_refused(lists);
   if (st != CKV_OK) return st;
   if (!table || !parent || !table_out || !refs || !taken || !length != !length_out) return CKV_EINVAL;
-  if (table == table_out || (length && length == length_out)) return CKV_EINVAL;
+  if (table == table_out || (length && (length == length_out || parent == length_out))) return CKV_EINVAL;
   return launch_fork(lists, table, parent, table_out, refs, taken, length, length_out, (hipStream_t)hip_stream) == hipSuccess ? CKV_OK : CKV_EHIP;
 }
 

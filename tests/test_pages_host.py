@@ -20,7 +20,7 @@ def _tree(**kw):
                                              g("lse", None), g("ws"), kw.get("ws_bytes", 1 << 40), None)
 
 
-def _sees(batch=2, n=5, parent=AT, start=AT, sees=AT, positions=AT):
+def _sees(batch=2, n=5, parent=AT, start=AT, sees=AT, positions=ALSO):
     return B.load().ckv_tree_sees(batch, n, parent, start, sees, positions, None)
 
 
@@ -73,7 +73,7 @@ def test_struct_layout_matches_the_header():
 
 
 def test_trees_are_refused():
-    for kw in (dict(batch=0), dict(n=0), dict(parent=None), dict(sees=None), dict(start=None), dict(sees=ctypes.c_void_p(4100))):
+    for kw in (dict(batch=0), dict(n=0), dict(parent=None), dict(sees=None), dict(start=None), dict(sees=ctypes.c_void_p(4100)), dict(positions=AT)):
         assert _sees(**kw) == B.CKV_EINVAL, kw
     assert _sees(n=4097) == B.CKV_EUNSUPPORTED
     assert _sees(batch=1 << 20, n=4096) == B.CKV_EUNSUPPORTED and _sees(batch=(1 << 22) + 1, n=1) == B.CKV_EUNSUPPORTED   # a launch's workgroups
@@ -103,6 +103,8 @@ def test_compact_refuses():
     assert _compact(kp=ODD) == B.CKV_EINVAL and _compact(vp=ODD) == B.CKV_EINVAL
     assert _compact(pages=None) == B.CKV_EINVAL and _compact(cap=0) == B.CKV_EINVAL
     assert _compact(length_out=AT) == B.CKV_EINVAL                                    # the lengths that are read
+    for name in ("length", "count", "kept"):
+        assert _compact(**{name: ALSO}) == B.CKV_EINVAL, name                         # what is written
     assert _compact(stride=(ctypes.c_int64 * 2)(-1, 0)) == B.CKV_EINVAL and _compact(stride=(ctypes.c_int64 * 2)(9, -9)) == B.CKV_EINVAL
     assert _compact(p=_params(d=96)) == B.CKV_EUNSUPPORTED
     assert _compact(p=_params(batch=(1 << 16) + 1, n_q_heads=4)) == B.CKV_EUNSUPPORTED   # a launch's workgroups
@@ -137,6 +139,7 @@ def test_calls_on_lists_refuse():
     for name in ("table", "parent", "out", "refs", "taken", "length", "length_out"):
         assert _fork(l, **{name: None}) == B.CKV_EINVAL, name                            # length without its output, too
     assert _fork(l, out=AT) == B.CKV_EINVAL and _fork(l, length_out=AT) == B.CKV_EINVAL  # in place
+    assert _fork(l, parent=ALSO) == B.CKV_EINVAL
     for name in ("table", "first", "end", "refs", "taken", "copy", "result"):
         assert _reserve(l, **{name: None}) == B.CKV_EINVAL, name
     assert _reserve(l, n=-1) == B.CKV_EINVAL and _reserve(l, n=1 << 30) == B.CKV_EUNSUPPORTED
