@@ -87,15 +87,18 @@ class Tensors {
   const at::Tensor &add_idx(PyObject *o, const ckv_params *p) {
     const at::Tensor *t = needed(o, "idx");
     bool ok = t->scalar_type() == at::kInt && (t->dim() == 2 || t->dim() == 3) && t->size(0) == p->batch && t->size(-1) > 0;
-    ok = ok && (t->size(-1) == 1 || t->stride(-1) == 1) && (t->dim() == 2 || t->size(1) == p->n_kv_heads);
+    ok = ok && t->size(-1) <= INT32_MAX && (t->size(-1) == 1 || t->stride(-1) == 1) && (t->dim() == 2 || t->size(1) == p->n_kv_heads);
     if (!ok) refuse("idx", at::kInt, {p->batch, p->n_kv_heads, t->dim() > 0 ? t->size(-1) : 0}, "(or without the heads' axis) with a contiguous last axis");
     return *t;
   }
-  // Of a tensor's own sizes, as many axes as `dims`; added by add() with them.
+  // Of a tensor's own sizes, as many axes as `dims`; added by add() with them. The library takes such a size as an int32.
   static const at::Tensor &sized(PyObject *o, const char *name, int64_t dims) {
     if (!THPVariable_Check(o) || THPVariable_Unpack(o).dim() != dims)
       throw std::invalid_argument(std::string(name) + " has to be a tensor of " + std::to_string(dims) + " axes");
-    return THPVariable_Unpack(o);
+    const at::Tensor &t = THPVariable_Unpack(o);
+    for (const int64_t size : t.sizes())
+      if (size > INT32_MAX) throw std::invalid_argument(std::string(name) + " has to be a tensor of axes below 2^31");
+    return t;
   }
   // Bytes, of any type.
   Py_ssize_t add_bytes(PyObject *o, const char *name) {

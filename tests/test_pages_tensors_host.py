@@ -70,6 +70,15 @@ def test_what_is_not_as_described_is_refused(by_head, name, calls, change):
             _calls(bad, by_head)[call]()
 
 
+def test_sizes_beyond_an_int32_are_refused():
+    many = lambda *s: torch.empty(*s, dtype=I32, device="meta")  # noqa: E731
+    for change, calls in ((dict(parent=many((1 << 32) + 2, 70)), ("sees",)), (dict(parent=many(2, (1 << 32) + 70)), ("sees",)),
+                          (dict(copy=many((1 << 32) + 5, 2)), ("copy", "reserve")), (dict(idx=many(2, (1 << 32) + 10)), ("compact",))):
+        for call in calls:
+            with pytest.raises(ValueError, match=f"^{next(iter(change))} has to be (?!on the GPU)"):
+                _calls(dict(_tensors(), **change), False)[call]()
+
+
 @pytest.mark.parametrize("by_head", [False, True])
 def test_what_is_in_order_is_refused_for_its_place_alone(by_head):
     good = _tensors()
