@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(ReserveArgs a)
     wait_vm_at_most<0>();
     __syncthreads();
   };
-  const int words = (a.to.n_pages + 31) / 32;
+  const int words = (a.to.n_pages - 1) / 32 + 1;
   auto free_bits = [&](int64_t w) CKV_INLINE {
     uint32_t bits = w < words ? ~a.to.taken[w] : 0u;
     if (w == words - 1 && a.to.n_pages % 32) bits &= (1u << a.to.n_pages % 32) - 1u;

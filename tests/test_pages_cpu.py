@@ -323,3 +323,21 @@ def _lists(path, c):
 @pytest.mark.parametrize("i", range(len(v.LISTS)))
 def test_lists_share_get_and_give_back_pages(lib_path, i):
     in_child(_lists, lib_path, v.LISTS[i])
+
+
+def _most_pages(path):
+    lib, n = cpu.load(path), 2 ** 31 - 1
+    l = B.CkvLists(1, 1, n, 16, 4, 0)
+    l.table_stride[0] = l.table_stride[1] = 4
+    table, copy, result = _at_fence(np.full((1, 4), -1, np.int32)), _at_fence(np.full((1, 2), 9, np.int32)), _at_fence(np.full(2, 9, np.int32))
+    refs, taken = np.zeros(n, np.int32), np.zeros(2 ** 26, np.uint32)   # only what is written takes memory
+    first, end = _at_fence(np.zeros((1, 1), np.int32)), _at_fence(np.full((1, 1), 40, np.int32))
+    taken[0] = 0xfffffffd
+    refs[0] = refs[2:32] = 1
+    assert lib.ckv_pages_reserve(ref(l), P(table), P(first), P(end), P(refs), P(taken), P(copy), 1, P(result), None) == B.CKV_OK
+    assert table.tolist() == [[1, 32, 33, -1]] and result.tolist() == [0, 0] and copy.tolist() == [[-1, -1]]
+    assert taken[:2].tolist() == [2 ** 32 - 1, 3] and refs[[1, 32, 33]].tolist() == [1, 1, 1]
+
+
+def test_as_many_pages_as_an_int32_holds(lib_path):
+    in_child(_most_pages, lib_path)
