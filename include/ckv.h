@@ -484,6 +484,7 @@ ckv_status ckv_paged_attention(const ckv_params *params, const ckv_pages *pages,
  * ckv_paged_tree_attention is ckv_paged_attention with these words in place of the causal order among the new tokens: token i < count sees the rows
  * j < length - count, and row length - count + t for t <= i where its bit t is set. Words of any origin do (a token without bits sees the rows in
  * front of the new ones alone, and one that sees no row gets zeros and lse = -inf); bits of tokens behind i are not looked at. n is 65536 at most.
+ * In bf16 the weights enter the second product off by 2^-16 of themselves in calls of any size, as in a one-token step.
  *   sees        in   [Bz,n,ceil(n/64)] 64-bit words, one set for all heads
  *   the others       as for ckv_paged_attention, the workspace too
  */

@@ -28,11 +28,13 @@ constexpr int kStageRows = 64;  // two blocks of 32 rows
 
 // A whole step in bf16, its instructions in the order that they are issued in: slot by slot a matrix product (the two kinds in turn), the operands
 // of those two or four slots further on, and a share of the softmax: first the maximum, then a few exponentials each. Left to itself the compiler puts
-// all products first, each behind a wait for its operand. `next` gets the logits of K's block, `weights` changes from the block before to z's.
-template <int DT, int DH>
+// all products first, each behind a wait for its operand. `next` gets the logits of K's block, `weights` change from the block before to z's.
+// TWO: the second product takes them in two terms, `rest` what the rounding of the first one leaves, with the first product's slot between the two.
+template <int DT, int DH, bool TWO>
 __device__ __forceinline__ void whole_step(const char *k_image, const char *v_image, int lane, const u32x4_d (&qf)[Image<DT, DH>::STEPS],
-                                           const f32x16_p &z, f32x16_p &next, Weights<DT> &weights, f32x16_p (&acc)[DH / 32], float scale2, Running &run) {
-  constexpr int STEPS = DH / 16, DTILES = DH / 32, SLOTS = 2 * STEPS, MAX_SLOTS = SLOTS / 4, EXP_SLOTS = SLOTS - MAX_SLOTS;
+                                           const f32x16_p &z, f32x16_p &next, Weights<DT> &weights, Weights<DT> &rest, f32x16_p (&acc)[DH / 32],
+                                           float scale2, Running &run) {
+  constexpr int STEPS = DH / 16, DTILES = DH / 32, KINDS = TWO ? 3 : 2, SLOTS = KINDS * STEPS, MAX_SLOTS = SLOTS / 4, EXP_SLOTS = SLOTS - MAX_SLOTS;
   constexpr int AHEAD = 2;
   static_assert(DT == CKV_BF16 && 2 * DTILES == STEPS, "as many products of one kind as of the other");
   const int k_at = k_lane<CKV_BF16, DH>(lane), v_at = v_lane<DH>(lane);
@@ -43,12 +45,12 @@ __device__ __forceinline__ void whole_step(const char *k_image, const char *v_im
     vf[i] = v_operand<DH>(v_image, v_at, i % DTILES, i / DTILES);
   }
   float mx = z[0], part[4], w[16];
-  Weights<DT> made;
+  Weights<DT> made, left;
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int slot = 0; slot < SLOTS; ++slot) {
-    const int i = slot / 2;
-    if (slot % 2 == 0) {
+    const int i = slot / KINDS, kind = TWO && slot % 3 < 2 ? 1 - slot % 3 : slot % KINDS;  // 0: the first product, 1, 2: a term of the second
+    if (kind == 0) {
       if (i + AHEAD < STEPS) kf[i + AHEAD] = k_operand(k_image, k_at, i + AHEAD);
       if (i == 0) {
 #pragma unroll
@@ -56,8 +58,8 @@ __device__ __forceinline__ void whole_step(const char *k_image, const char *v_im
       }
       mma_piece<CKV_BF16>(next, kf[i], qf[i]);
     } else {
-      if (i + AHEAD < STEPS) vf[i + AHEAD] = v_operand<DH>(v_image, v_at, (i + AHEAD) % DTILES, (i + AHEAD) / DTILES);
-      mma_piece<CKV_BF16>(acc[i % DTILES], vf[i], weights.piece[i / DTILES]);
+      if (kind == 1 && i + AHEAD < STEPS) vf[i + AHEAD] = v_operand<DH>(v_image, v_at, (i + AHEAD) % DTILES, (i + AHEAD) / DTILES);
+      mma_piece<CKV_BF16>(acc[i % DTILES], vf[i], (kind == 1 ? weights : rest).piece[i / DTILES]);
     }
     if (slot < MAX_SLOTS) {
 #pragma unroll
@@ -68,13 +70,18 @@ __device__ __forceinline__ void whole_step(const char *k_image, const char *v_im
       for (int r = (slot - MAX_SLOTS) * 16 / EXP_SLOTS; r < (slot - MAX_SLOTS + 1) * 16 / EXP_SLOTS; ++r) {
         w[r] = __builtin_amdgcn_exp2f(fmaf(z[r], scale2, -run.ref));
         part[r % 4] = r < 4 ? w[r] : part[r % 4] + w[r];
-        if (r % 2) made.piece[r / 8][r / 2 % 4] = pack_bf16(w[r - 1], w[r]);
+        if (r % 2) {
+          const uint32_t both = pack_bf16(w[r - 1], w[r]);
+          made.piece[r / 8][r / 2 % 4] = both;
+          if (TWO) left.piece[r / 8][r / 2 % 4] = rest_of(w[r - 1], w[r], both);
+        }
       }
     }
     __builtin_amdgcn_sched_barrier(0);
   }
   run.sum += (part[0] + part[1]) + (part[2] + part[3]);
   weights = made;
+  if (TWO) rest = left;
 }
 
 // Waves of a tile's kernel that a SIMD holds, for its __launch_bounds__.
@@ -87,6 +94,7 @@ constexpr int tile_occupancy(int dt, int d, int waves) { return waves == 4 && dt
 template <int DT, int DH, int WAVES, int GROUPS, class Args>
 __device__ __forceinline__ void attend_tile(const Args &a) {
   constexpr bool TREE = std::is_same<Args, TreeArgs>::value;
+  constexpr bool TWO = TREE && DT == CKV_BF16;  // terms of the weights in the second product
   typedef Image<DT, DH> I;
   constexpr int BYTES = kStageRows * I::ROW;
   constexpr int MEMBERS = WAVES / GROUPS;           // waves of a group
@@ -243,25 +251,27 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
     fetch_k(first);
     fetch_sees(first);
     f32x16_p z;           // logits of the block in work
-    Weights<DT> weights;  // of the one before
+    Weights<DT> weights, rest;  // of the one before
     // Steps of the pipeline: the first product of a block, the softmax of the one before, the second product of the one before that, none
     // of which waits for another: the matrix cores have work while the vector units are at the softmax. What is a branch comes in
     // front, so that the rest is one block of instructions to be scheduled.
     auto softmax = [&]() CKV_INLINE {
       to_weights<false>(z, a.scale2, run, kFinite);
       weights = as_operand<DT>(z);
+      if constexpr (TWO) rest = rest_of(z, weights);
     };
     auto step = [&](const char *k_image, int z_row, const char *v_image, int stage) CKV_INLINE {
       rescale(acc, run);
       hide(z, z_row, stage);
       f32x16_p next;
       if constexpr (DT == CKV_BF16) {
-        whole_step<DT, DH>(k_image, v_image, lane, qf, z, next, weights, acc, a.scale2, run);
+        whole_step<DT, DH, TWO>(k_image, v_image, lane, qf, z, next, weights, rest, acc, a.scale2, run);
       } else {
         first_product<DT, DH>(k_image, lane, qf, next);
         second_product<DT, DH, false>(v_image, lane, weights, acc, kFinite);
         softmax();
       }
+      if constexpr (TWO) pin(rest, run.sum);
       pin(weights, run.sum);  // or the exponentials move behind the next step's branch, away from these products
       z = next;
     };
@@ -298,11 +308,13 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
     advance(own_last);
     const char *v = s_v[(own_last - 1 - first) & 1];
     rescale(acc, run);
-    second_product<DT, DH, false>(v, lane, weights, acc, kFinite);
+    if constexpr (TWO) second_product<DT, DH, false>(v, lane, weights, acc, kFinite, rest);
+    else second_product<DT, DH, false>(v, lane, weights, acc, kFinite);
     hide(z, own_last * kStageRows - 32, own_last);
     softmax();
     rescale(acc, run);
-    second_product<DT, DH, false>(v + HALF, lane, weights, acc, kFinite);
+    if constexpr (TWO) second_product<DT, DH, false>(v + HALF, lane, weights, acc, kFinite, rest);
+    else second_product<DT, DH, false>(v + HALF, lane, weights, acc, kFinite);
     for (stage = own_last + 1; stage <= last; ++stage) advance(stage);  // the other waves' rows, and all barriers
   }
   if (GROUPS > 1 && last - first < most)
@@ -335,7 +347,9 @@ __device__ __forceinline__ void attend_tile(const Args &a) {
           hide(z, stage * kStageRows + 32 * k, -1);
           to_weights<true>(z, a.scale2, run, mode, room);
           if (mode == kFinite) rescale(acc, run);  // marks are counted, whatever the row behind them weighs
-          second_product<DT, DH, true>(s_v[(stage - first) & 1] + k * HALF, lane, as_operand<DT>(z), acc, mode);
+          const Weights<DT> operand = as_operand<DT>(z);
+          if constexpr (TWO) second_product<DT, DH, true>(s_v[(stage - first) & 1] + k * HALF, lane, operand, acc, mode, rest_of(z, operand));
+          else second_product<DT, DH, true>(s_v[(stage - first) & 1] + k * HALF, lane, operand, acc, mode);
         }
       }
       take_marks(marks, acc, mode);

@@ -110,6 +110,16 @@ def attention(c, s):
     return out, out_tol, lse, lse_tol
 
 
+def fine(c):
+    """A bf16 case, its results and the bound on them with weights that are off by 2^-16 of themselves at most (two bf16 terms: each is off by 2^-8 of what
+    it stands for), in place of one rounding to bf16: attention()'s without its 2^-8 of sum_j w_j |v_j|."""
+    s = u.make(c)
+    want, tol, lse, lse_tol = attention(c, s)
+    plain = dict(s, v_pages=u.stored(np.abs(u.values(np.ascontiguousarray(s["v_pages"]))), c["dtype"]))
+    size = np.nan_to_num(attention(c, plain)[0])   # sum_j w_j |v_j|; no rows of the call: 0
+    return s, want, tol - (u.H8 - 2.0 ** -16) * size, lse, lse_tol
+
+
 TREES = [
     tree_case(n=1, lengths=((1, 1), (2, 70), (0, 5))),
     tree_case(n=16, heads=(8, 2), lengths=((90, 60), (16, 17)), by_head=True, page=32),

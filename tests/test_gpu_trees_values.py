@@ -1,9 +1,11 @@
 """Attention of trees over pages, on the GPU, of values that are not finite or nearly so (paged_values makes them, pages_util the results in 64 bits)."""
+import numpy as np
 import pytest
 import torch
 
 import paged_values as pv
 import pages_util as v
+from test_gpu_paged import host
 from test_gpu_pages import attend, check, tree_on_gpu
 import paged_util as u
 
@@ -43,3 +45,13 @@ def test_drafted_tokens_that_are_not_finite(c, far_away):
 @pytest.mark.parametrize("c", TREES, ids=range(len(TREES)))
 def test_a_mean_of_large_values_is_finite(c, rise, value, sign, infinite):
     _run(c, pv.high(c, rise, value, sign, infinite))
+
+
+@pytest.mark.parametrize("c", [c for c in v.TREES + v.MANY if c["dtype"] == "bf16"], ids=lambda c: f"{c['Hq']}x{c['n']}")
+def test_trees_lose_nothing_to_the_weights(c):
+    s, want, tol, want_lse, lse_tol = v.fine(c)
+    out, lse = attend(c, tree_on_gpu(c, s))
+    torch.cuda.synchronize()
+    old = np.arange(c["n"]) >= np.repeat(u.new_counts(c), c["Hq"] // c["Hkv"], 1)[..., None]
+    u.check(host(out), np.where(old[..., None], 9.0, want), tol, "out")
+    u.check(host(lse), np.where(old, 9.0, want_lse), lse_tol, "lse")

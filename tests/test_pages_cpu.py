@@ -78,6 +78,19 @@ def test_attention_of_trees(lib_path, i):
     in_child(_tree, lib_path, v.TREES[i])
 
 
+def _tree_fine(path, c):
+    s, want, tol, wl, lt = v.fine(c)
+    out, lse = _attend(cpu.load(path), c, _fenced(s))
+    old = np.arange(c["n"]) >= np.repeat(u.new_counts(c), c["Hq"] // c["Hkv"], 1)[..., None]
+    u.check(out, np.where(old[..., None], 9.0, want), tol, "out")
+    u.check(lse, np.where(old, 9.0, wl), lt, "lse")
+
+
+@pytest.mark.parametrize("i", [1, 4, 5, 8, 9, 18, 19])
+def test_trees_lose_nothing_to_the_weights(lib_path, i):
+    in_child(_tree_fine, lib_path, v.TREES[i])
+
+
 def _tree_odd(path, c, kind):
     lib, s = cpu.load(path), u.make(c)
     if kind == "bad_pages":
