@@ -479,7 +479,7 @@ ckv_status ckv_paged_attention(const ckv_params *params, const ckv_pages *pages,
  *   parent      in   [batch,n] int32; a value that is not one of 0 .. i - 1 makes token i a root
  *   start       in   [batch] int32: a root's position; may be NULL with positions
  *   sees        out  [batch,n,ceil(n/64)] 64-bit words
- *   positions   out  [batch,n] int32, what ckv_norm_rotate and ckv_paged_append take, or NULL; not `parent` itself
+ *   positions   out  [batch,n] int32, what ckv_norm_rotate and ckv_paged_append take, or NULL; overlaps neither `parent` nor `start`
  *
  * ckv_paged_tree_attention is ckv_paged_attention with these words in place of the causal order among the new tokens: token i < count sees the rows
  * j < length - count, and row length - count + t for t <= i where its bit t is set. Words of any origin do (a token without bits sees the rows in
@@ -510,7 +510,7 @@ ckv_status ckv_paged_tree_attention(const ckv_params *params, const ckv_pages *p
  *   kept        in   [Bz,Hkv] int32
  *   k_pages, v_pages  in/out; pages that are written are in no other list, or other lists see the change (ckv_pages_reserve gives lists pages of
  *                    their own)
- *   length_out  out  [Bz,Hkv] int32, not `length`, `count` or `kept` itself
+ *   length_out  out  [Bz,Hkv] int32, overlaps none of `length`, `count` and `kept`
  */
 ckv_status ckv_paged_compact(const ckv_params *params, const ckv_pages *pages, const int32_t *table, const int32_t *length, const int32_t *count,
                              const int32_t *idx, const int64_t *idx_stride, int32_t cap, const int32_t *kept, void *k_pages, void *v_pages,
@@ -551,7 +551,7 @@ typedef struct {
  *   table       in   int32, table_stride        table_out  in/out  int32, table_stride, not overlapping `table`
  *   parent      in   [batch] int32
  *   length      in   [batch,n_kv_heads] int32, or NULL with length_out
- *   length_out  out  length[parent[b]], or 0 without one; not `length` or `parent` itself
+ *   length_out  out  length[parent[b]], or 0 without one; overlaps neither `length` nor `parent`
  */
 ckv_status ckv_pages_fork(const ckv_lists *lists, const int32_t *table, const int32_t *parent, int32_t *table_out, int32_t *refs,
                           uint32_t *taken, const int32_t *length, int32_t *length_out, void *hip_stream);

@@ -686,6 +686,12 @@ static bool misaligned(std::initializer_list<const void *> pointers) {
   return all & 15;
 }
 
+// Whether n entries at a and m at b have memory in common (no memory, null, has none).
+static bool meet(const int32_t *a, int64_t n, const int32_t *b, int64_t m) {
+  const uintptr_t p = (uintptr_t)a, q = (uintptr_t)b;
+  return a && b && p < q + 4 * (uintptr_t)m && q < p + 4 * (uintptr_t)n;
+}
+
 extern "C" ckv_status ckv_norm_rotate(const ckv_params *params, const ckv_rotation *rotation, const void *q, const void *k,
                                       const int32_t *positions, const float *inv_freq, const void *q_weight, const void *k_weight,
                                       const int32_t *count, void *q_out, void *k_out, void *hip_stream) {
@@ -790,8 +796,10 @@ extern "C" ckv_status ckv_paged_tree_attention(const ckv_params *params, const c
 
 extern "C" ckv_status ckv_tree_sees(int32_t batch, int32_t n, const int32_t *parent, const int32_t *start, uint64_t *sees, int32_t *positions,
                                     void *hip_stream) {
-  if (batch < 1 || n < 1 || !parent || !sees || ((uintptr_t)sees & 7) || (positions && !start) || positions == parent) return CKV_EINVAL;
+  if (batch < 1 || n < 1 || !parent || !sees || ((uintptr_t)sees & 7) || (positions && !start)) return CKV_EINVAL;
   if (n > kMostDrafts || tree_workgroups(batch, n) > kMostPagedWorkgroups) return CKV_EUNSUPPORTED;
+  const int64_t tokens = (int64_t)batch * n;
+  if (meet(positions, tokens, parent, tokens) || meet(positions, tokens, start, batch)) return CKV_EINVAL;  // which other workgroups read
   return launch_tree_sees(batch, n, parent, start, sees, positions, (hipStream_t)hip_stream) == hipSuccess ? CKV_OK : CKV_EHIP;
 }
 
@@ -801,7 +809,8 @@ extern "C" ckv_status ckv_paged_compact(const ckv_params *params, const ckv_page
   ckv_status st = validate(params);
   if (st != CKV_OK) return st;
   if (!table || !length || !idx || !kept || !k_pages || !v_pages || !length_out || cap < 1) return CKV_EINVAL;
-  if (length_out == length || length_out == count || length_out == kept) return CKV_EINVAL;  // a list's workgroups read these, one of them writes
+  const int64_t lists = (int64_t)params->batch * params->n_kv_heads;  // a list's workgroups read these, one of them writes
+  if (meet(length_out, lists, length, lists) || meet(length_out, lists, count, lists) || meet(length_out, lists, kept, lists)) return CKV_EINVAL;
   if (misaligned({k_pages, v_pages})) return CKV_EINVAL;
   if (idx_stride && (idx_stride[0] < 0 || idx_stride[1] < 0)) return CKV_EINVAL;
   st = pages_refused(params, pages);
@@ -845,7 +854,8 @@ extern "C" ckv_status ckv_pages_fork(const ckv_lists *lists, const int32_t *tabl
   const ckv_status st = lists_refused(lists);
   if (st != CKV_OK) return st;
   if (!table || !parent || !table_out || !refs || !taken || !length != !length_out) return CKV_EINVAL;
-  if (table == table_out || (length && (length == length_out || parent == length_out))) return CKV_EINVAL;
+  const int64_t rows = (int64_t)lists->batch * lists->n_kv_heads;
+  if (table == table_out || meet(length_out, rows, length, rows) || meet(length_out, rows, parent, lists->batch)) return CKV_EINVAL;
   return launch_fork(lists, table, parent, table_out, refs, taken, length, length_out, (hipStream_t)hip_stream) == hipSuccess ? CKV_OK : CKV_EHIP;
 }
 

@@ -79,6 +79,26 @@ def test_trees_are_refused():
     assert _sees(batch=1 << 20, n=4096) == B.CKV_EUNSUPPORTED and _sees(batch=(1 << 22) + 1, n=1) == B.CKV_EUNSUPPORTED   # a launch's workgroups
 
 
+def test_outputs_that_lie_where_other_workgroups_read():
+    """Wholly or in part: a sequence's positions, a list's length are written while another one's inputs have still to be read."""
+    at = lambda n: ctypes.c_void_p(1 << 16 | 4 * n)  # noqa: E731
+    far = ctypes.c_void_p(1 << 20)
+    for n, batch in ((5, 2), (700, 3)):
+        assert _sees(batch, n, far, at(0), AT, at(0)) == B.CKV_EINVAL                                             # positions where start is
+        for k in (1 - batch, batch * n - 1):
+            assert _sees(batch, n, far, at(batch + k), AT, at(batch)) == B.CKV_EINVAL                              # ... its last, its first entry
+        for k in (1 - batch * n, 0, batch * n - 1):
+            assert _sees(batch, n, at(3 * batch * n + k), far, AT, at(3 * batch * n)) == B.CKV_EINVAL               # where parent is
+    for name in ("length", "count", "kept"):
+        for k in (-3, 0, 3):                                                                                       # of 2 x 2 entries
+            assert _compact(**{name: at(8 + k)}, length_out=at(8)) == B.CKV_EINVAL, name
+    l = _lists()
+    for k in (-5, 0, 5):                                                                                           # of 3 x 2
+        assert _fork(l, length=at(8 + k), length_out=at(8)) == B.CKV_EINVAL
+    for k in (-2, 0, 5):
+        assert _fork(l, parent=at(8 + k), length_out=at(8)) == B.CKV_EINVAL
+
+
 def test_tree_attention_refuses():
     for name in ("q", "kp", "vp", "table", "length", "out", "sees"):
         assert _tree(**{name: None}) == B.CKV_EINVAL, name
