@@ -509,7 +509,7 @@ ckv_status ckv_paged_tree_attention(const ckv_params *params, const ckv_pages *p
  *   cap         entries of a list in idx, >= 1
  *   kept        in   [Bz,Hkv] int32
  *   k_pages, v_pages  in/out; pages that are written are in no other list, or other lists see the change (ckv_pages_reserve gives lists pages of
- *                    their own)
+ *                    their own). Heads with a list in common have rows of their own (with table_stride[1] = 0 neither head stride is 0)
  *   length_out  out  [Bz,Hkv] int32, overlaps none of `length`, `count` and `kept`
  */
 ckv_status ckv_paged_compact(const ckv_params *params, const ckv_pages *pages, const int32_t *table, const int32_t *length, const int32_t *count,

@@ -815,6 +815,8 @@ extern "C" ckv_status ckv_paged_compact(const ckv_params *params, const ckv_page
   if (idx_stride && (idx_stride[0] < 0 || idx_stride[1] < 0)) return CKV_EINVAL;
   st = pages_refused(params, pages);
   if (st != CKV_OK) return st;
+  // one list, one row for all heads: each head's workgroups would move what another's have moved
+  if (params->n_kv_heads > 1 && pages->table_stride[1] == 0 && (pages->k_stride[1] == 0 || pages->v_stride[1] == 0)) return CKV_EINVAL;
   Shape s;
   derive(params, &s);
   if ((int64_t)s.Bz * s.Hkv > kMostCompactLists) return CKV_EUNSUPPORTED;

@@ -131,6 +131,15 @@ def test_compact_refuses():
     assert _compact(pages=_pages(page_rows=24)) == B.CKV_EUNSUPPORTED and _compact(pages=_pages(k_stride=(2, 64))) == B.CKV_EINVAL
 
 
+def test_rows_of_one_head_under_one_list_do_not_move():
+    """Every head would move the same rows, the second one those that the first has moved."""
+    one = dict(table_stride=(1, 0))
+    assert _compact(pages=_pages(k_stride=(1, 0), v_stride=(1, 0), **one)) == B.CKV_EINVAL
+    assert _compact(pages=_pages(k_stride=(1, 0), **one)) == B.CKV_EINVAL and _compact(pages=_pages(v_stride=(1, 0), **one)) == B.CKV_EINVAL
+    for fine in (dict(k_stride=(1, 0), table_stride=(1, 50)), one):   # lists of their own; pages that hold every head: as far as the next refusal
+        assert _compact(pages=_pages(page_rows=24, **fine)) == B.CKV_EUNSUPPORTED, fine
+
+
 def test_copy_refuses():
     for name in ("copy", "kp", "vp"):
         assert _copy(**{name: None}) == B.CKV_EINVAL, name
