@@ -43,7 +43,7 @@ ckv_status validate(const ckv_params *p) {
     if (p->q_stride[i] % per16 || p->k_stride[i] % per16 || p->v_stride[i] % per16) return CKV_EINVAL;
   if (p->head_dim != 64 && p->head_dim != 128) return CKV_EUNSUPPORTED;
   if (p->window > kMaxWindowTiles * kTile) return CKV_EUNSUPPORTED;
-  if ((int64_t)p->batch * p->n_kv_heads > 65535) return CKV_EUNSUPPORTED;  // grid.y
+  if ((int64_t)p->batch * p->n_kv_heads > kMostUnits) return CKV_EUNSUPPORTED;
   if (p->seq_len > (1 << 24)) return CKV_EUNSUPPORTED;
   // the staged scan addresses the 32 rows of a key tile with 32-bit offsets
   if (p->k_stride[2] * (int64_t)(p->dtype == CKV_BF16 ? 2 : 4) * kTile >= ((int64_t)1 << 31)) return CKV_EUNSUPPORTED;
@@ -819,7 +819,6 @@ extern "C" ckv_status ckv_paged_compact(const ckv_params *params, const ckv_page
   if (params->n_kv_heads > 1 && pages->table_stride[1] == 0 && (pages->k_stride[1] == 0 || pages->v_stride[1] == 0)) return CKV_EINVAL;
   Shape s;
   derive(params, &s);
-  if ((int64_t)s.Bz * s.Hkv > kMostCompactLists) return CKV_EUNSUPPORTED;
   if (launch_compact(s, pages, table, length, count, idx, idx_stride, cap, kept, k_pages, v_pages, length_out, (hipStream_t)hip_stream) != hipSuccess)
     return CKV_EHIP;
   return CKV_OK;

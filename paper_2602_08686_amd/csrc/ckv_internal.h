@@ -21,6 +21,7 @@ constexpr int kScoreWaves = 4;     // waves per workgroup in the scan kernels
 // split of the key axis, and with it the workspace layout, must be the same for ckv_workspace_bytes
 // (which may run where no device is visible) and for the calls that use the workspace.
 constexpr int kComputeUnits = 256;
+constexpr int kMostUnits = 65535;   // batch elements times KV heads: grid.y
 constexpr int kSelectThreads = 1024;
 // Geometry of the fused utility form of the scan's second pass (ckv_scan.h). It works in rounds of
 // kRing * kTile keys per wave; each round writes the utilities of the kRing * kTile keys that end

@@ -124,6 +124,7 @@ hipError_t launch_compact(const Shape &s, const ckv_pages *pages, const int32_t 
   a.pieces = (int64_t)cap * 2 * a.row_pieces <= 1024 ? 2 * a.row_pieces : 8;
   if (a.pieces == 8 && cap > 1024 && (int64_t)s.Bz * s.Hkv * a.row_pieces / 4 <= kComputeUnits / 4) a.pieces = 4;
   a.splits = 2 * a.row_pieces / a.pieces;
+  static_assert(kMostUnits * 16ll * 1024 < 1ll << 32, "a list has 16 workgroups of 1024 threads at most, a launch fewer than 2^32 threads");
   int threads = 1024;
   while (threads > 64 && (int64_t)cap * a.pieces <= threads / 2) threads /= 2;
   const dim3 grid((unsigned)(s.Bz * s.Hkv * a.splits));

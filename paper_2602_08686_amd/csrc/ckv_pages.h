@@ -65,7 +65,6 @@ int64_t tree_workgroups(int batch, int n);
 hipError_t launch_tree_sees(int batch, int n, const int32_t *parent, const int32_t *start, uint64_t *sees, int32_t *positions, hipStream_t stream);
 
 // Rows and pages that move.
-constexpr int kMostCompactLists = 1 << 17;  // a list has 16 workgroups of 1024 threads at most, and those of a launch have to be fewer than 2^32
 hipError_t launch_compact(const Shape &s, const ckv_pages *pages, const int32_t *table, const int32_t *length, const int32_t *count,
                           const int32_t *idx, const int64_t *idx_stride, int cap, const int32_t *kept, void *k_pages, void *v_pages,
                           int32_t *length_out, hipStream_t stream);
