@@ -561,8 +561,11 @@ ckv_status ckv_pages_fork(const ckv_lists *lists, const int32_t *table, const in
  * one of their own, with a pair (former page, new page) in `copy` for ckv_pages_copy on each pool. Where all that share a page ask for it, the
  * last of them keeps it. New pages are the lowest-numbered free ones, in the order of the entries (batch, KV head, entry), pairs are in that order too.
  * All or nothing: where there are too few free pages or too few places for pairs, only copy (no pairs) and result are written.
- *   first, end  in   [batch,n_kv_heads] int32; nothing to do where end <= first, or behind max_pages * page_rows
- *   copy        out  [n_copy,2] int32, pairs and behind them -1; n_copy >= 0 (copy may be NULL with 0)
+ *   first, end  in   [batch,n_kv_heads] int32; nothing to do where end <= first, or behind max_pages * page_rows. Heads that have a list in common: one range,
+ *                    from the least first to the greatest end of those with rows to come, whatever lies between. Where such heads are of very different lengths
+ *                    (rows that retention kept by head), pages between their rows get copies too if lists share them; a list for every head avoids it
+ *   copy        out  [n_copy,2] int32, pairs and behind them -1; n_copy >= 0 (copy may be NULL with 0). Never more pairs than shared pages in those ranges,
+ *                    (end - 1) / page_rows - first / page_rows + 1 pages of a list at most
  *   result      out  [2] int32: pages (or places for pairs, if that is more) that are missing, 0 if all is done; pairs
  */
 ckv_status ckv_pages_reserve(const ckv_lists *lists, int32_t *table, const int32_t *first, const int32_t *end, int32_t *refs, uint32_t *taken,

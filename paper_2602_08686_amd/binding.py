@@ -496,7 +496,8 @@ def ckv_pages_fork(lists, table, parent, table_out, refs, taken, length=None, le
 
 
 def ckv_pages_reserve(lists, table, first, end, refs, taken, copy, result, stream=None):
-    """first, end [Bz,Hkv] int32; copy [n,2] int32 or None; result [2] int32."""
+    """first, end [Bz,Hkv] int32 (heads with a list in common: one range, from the least first to the greatest end); copy [n,2] int32 or None;
+    result [2] int32."""
     device, stream = _place(stream)
     at = load_tensors().pages_reserve(lists, device, table, first, end, refs, taken, copy, result)
     _check(load().ckv_pages_reserve(ctypes.byref(lists), *at, stream), "ckv_pages_reserve")
