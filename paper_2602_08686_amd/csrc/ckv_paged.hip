@@ -87,32 +87,42 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedArgs a)
 // themselves 24.1 / 19.5 / 19.5; f32, heads of 64, 101 tokens, 523 rows (64 / 128) 24.3 / 29.6. One chunk up to 1024 (bf16) or 256 (f32) rows
 // of few columns: 500 rows 10.1, two chunks 11.0; batch 16, 544 rows 10.7, two chunks 11.6, 1000 rows 16.9, two 16.3; but batch 4 over 2000 rows
 // 23.7 with one, 12.6 with the rule's.
-// For trees, bf16. Tiles of 256 columns where the rows are more than the caches hold, as each tile reads them, and hardly any column is there for nothing:
-// us, 128 / 256 columns: 60 tokens, batch 4, 32768 rows, 512 MiB 192 / 172, 8192 rows 57.7 / 54.7, 500 tokens, batch 2, 32771 rows 573 / 538, 8195 rows
-// 161 / 156, 4099 rows, 32 MiB 94.4 / 94.5, 2099 rows 61.2 / 64.4, but 328 columns (384 / 512), 9312 rows 47.5 / 50.0. Otherwise tiles of 128 by two groups
-// of four waves, where that leaves about as many waves busy as workgroups of four would be: 150 tiles on 256 CUs, batch 3, 9068 rows 73 in 450 workgroups of
-// four waves, 108 in 150 of eight; and not for the few stages of short lists, 180 rows 13.9 / 14.4.
-constexpr int64_t kRowsInCaches = 48 << 20;
+// For trees, bf16. Tiles of 256 columns, which read a row once where two of 128 read it twice, where hardly any column is there for nothing, about as many
+// waves stay busy (a list has 64 chunks at most) and a chunk is so long that its rows outweigh its start and end: 1024 rows of 128, or six times as many
+// where tiles of 128 need no chunks, and so no merge. us, 128 / 256 columns: 60 tokens, batch 4, 32768 rows 235 / 217, 8192 (chunks of 1024) 74 / 70, 6144
+// 58.6 / 58.6, 4096 43.5 / 46.1; 32/8 heads, one sequence, 32768 rows (1024) 71.8 / 70.1, 16384 43.0 / 46.5; 500 tokens, batch 2, 32771 rows 767 / 722, and, 128
+// in one chunk, 12288 (6144) 305 / 295, 8195 199 / 207; heads of 64, batch 4, 16384 rows 78.5 / 76.9, 8192 43.6 / 44.9. Workgroups of eight waves: 8/1 heads, 32
+// tokens, 131072 rows 62 in 128 / 91 in 64; 16/2 heads, 65536 rows 47 in 256 / 58 in 128; 24/3 heads, 131072 rows 101.6 in 252 / 101.5 in 192. 328
+// columns (384 / 512), batch 8, 9312 rows 58.9 / 63.5. Otherwise tiles of 128 by two groups of four waves, where that leaves about as many waves busy as
+// workgroups of four would be: 150 tiles on 256 CUs, batch 3, 9068 rows 178 in 450 workgroups of four waves, 221 in 150 of eight; and not for the few stages of
+// short lists, 180 rows 14.8 / 15.8.
+constexpr int64_t kFarRow = 1024 * 128;  // components of a row times rows of a chunk
 PagedPlan plan_paged(const Shape &s, int n_rows, bool tree) {
   PagedPlan p;
   const bool bf16 = s.esize == 2;
   const int64_t units = (int64_t)s.Bz * s.Hkv, cols = (int64_t)s.G * s.T;
   p.by_rows = cols <= (bf16 ? kMostRowsCols : kMostRowsColsF32);
-  const int64_t narrow = (cols + 127) / 128 * 128, wide = (cols + 255) / 256 * 256;  // columns that the products are made for
-  const bool far = tree && bf16 && wide * 20 <= narrow * 21 && units * n_rows * s.d * 2 * s.esize > kRowsInCaches;
-  const int waves = units * ((cols + 255) / 256) >= kComputeUnits || far ? 8 : 4;
+  const int least = p.by_rows ? (bf16 ? 256 : 128) : bf16 ? 512 : s.d == 64 ? 64 : 128;
+  const int64_t most = p.by_rows && n_rows <= (bf16 ? 1024 : 256) ? 1 : (n_rows + least - 1) / least;
+  const auto chunks_of = [&](int64_t tiles, int64_t places) { return std::min<int64_t>({places / tiles, most, kMostChunks}); };
+  const int64_t narrow = units * ((cols + 127) / 128), wide = units * ((cols + 255) / 256);  // tiles
+  bool far = tree && bf16 && !p.by_rows && wide <= kComputeUnits && wide * 2 * 20 <= narrow * 21;
+  if (far) {
+    const int64_t of_wide = chunks_of(wide, kComputeUnits), of_narrow = chunks_of(narrow, kComputeUnits);
+    const int64_t busy = narrow <= kComputeUnits ? narrow * of_narrow : narrow / 2;  // in workgroups of eight waves
+    far = 4 * wide * of_wide >= 3 * busy && (int64_t)n_rows * s.d >= of_wide * kFarRow * (of_wide > 1 && of_narrow == 1 ? 6 : 1);
+  }
+  const int waves = wide >= kComputeUnits || far ? 8 : 4;
   p.tile_cols = p.by_rows ? kRowsCols : waves * 32;
   p.stage_rows = p.by_rows ? 32 : kStageRows;
   p.col_tiles = (int)((cols + p.tile_cols - 1) / p.tile_cols);
   const int64_t tiles = units * p.col_tiles;
   const bool two = !p.by_rows && waves == 4 && (bf16 || s.d == 64 || n_rows < 1024);
   int64_t chunks = (two ? 2 : 1) * kComputeUnits / tiles;
-  const int least = p.by_rows ? (bf16 ? 256 : 128) : bf16 ? 512 : s.d == 64 ? 64 : 128;
-  const int64_t most = p.by_rows && n_rows <= (bf16 ? 1024 : 256) ? 1 : (n_rows + least - 1) / least;
   if (chunks > most) chunks = most;
   if (chunks > kMostChunks) chunks = kMostChunks;
   if (chunks < 1) chunks = 1;
-  const int64_t pairs = std::min<int64_t>({kComputeUnits / tiles, most, kMostChunks});
+  const int64_t pairs = chunks_of(tiles, kComputeUnits);
   p.halves = tree && bf16 && !p.by_rows && waves == 4 && pairs > 0 && 11 * pairs >= 5 * chunks && n_rows > 4 * kStageRows;
   if (p.halves) chunks = pairs;
   p.n_chunks = (int)chunks;

@@ -90,7 +90,7 @@ constexpr int tile_occupancy(int dt, int d, int waves) { return waves == 4 && dt
 // Args: PagedArgs, or TreeArgs, whose tokens see of the new ones what their words say. GROUPS = 2: half of the
 // waves take the first half of the chunk's stages, the others the second half, for the same columns, each with buffers of its own, and they are joined
 // in LDS: as many waves as two workgroups, whose sums would go through memory and a launch. us, bf16, two workgroups / groups: 500 tokens, 32/8 heads,
-// batch 2, 4099 rows 94 / 84, 563 rows 39 / 27, 59 tokens, heads of 64, batch 12, 793 rows 24.6 / 19.0, 41 tokens, 16/2 heads, batch 8, 9312 rows 47.6 / 45.4.
+// batch 2, 4099 rows 117 / 106, 563 rows 37.5 / 28.6, 59 tokens, heads of 64, batch 12, 793 rows 27.7 / 21.5, 41 tokens, 16/2 heads, batch 8, 9312 rows 60.0 / 57.7.
 template <int DT, int DH, int WAVES, int GROUPS, class Args>
 __device__ __forceinline__ void attend_tile(const Args &a) {
   constexpr bool TREE = std::is_same<Args, TreeArgs>::value;

@@ -2,8 +2,8 @@
 // new tokens. Rows in front of them are seen by all, so the mask is looked at in the blocks of 32 rows that hold new ones alone: a column's 32 bits
 // of such a block are two words of its token's, shifted, as the new rows begin anywhere in a block. The words come into LDS as rows do, ahead of their block.
 // Weights in bf16 enter the second product in two terms, for many columns too, so that a token's result is as near to 64 bits as that of a one-token step.
-// Measured, bf16, 32/8 heads of 128: 16 tokens of 16 sequences over up to 560 rows a head 13.9 us (a token 11.4), 60 tokens, batch 4, 32768 rows 170 us, 757
-// TFLOP/s of the visible pairs' products, 500 tokens, batch 2, 4099 rows 84 us, 702; f32, 14/2 heads of 64, 33 tokens, 1501 rows 18.1 us.
+// Measured, bf16, 32/8 heads of 128: 16 tokens of 16 sequences over up to 560 rows a head 13.9 us (a token 11.4), 60 tokens, batch 4, 32768 rows 217 us, 593
+// TFLOP/s of the visible pairs' products, 500 tokens, batch 2, 4099 rows 105 us, 566; f32, 14/2 heads of 64, 33 tokens, 1501 rows 18.1 us.
 #include "ckv_paged_few.h"
 #include "ckv_paged_tile.h"
 

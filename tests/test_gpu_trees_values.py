@@ -47,11 +47,26 @@ def test_a_mean_of_large_values_is_finite(c, rise, value, sign, infinite):
     _run(c, pv.high(c, rise, value, sign, infinite))
 
 
-@pytest.mark.parametrize("c", [c for c in v.TREES + v.MANY if c["dtype"] == "bf16"], ids=lambda c: f"{c['Hq']}x{c['n']}")
-def test_trees_lose_nothing_to_the_weights(c):
+def _fine(c, entries=0):
+    """entries: of a list at least, as in a call that is planned for long lists."""
     s, want, tol, want_lse, lse_tol = v.fine(c)
+    more = max(0, entries - s["table"].shape[-1])
+    s["table"] = np.concatenate([s["table"], np.full(s["table"].shape[:-1] + (more,), -1, np.int32)], -1)
     out, lse = attend(c, tree_on_gpu(c, s))
     torch.cuda.synchronize()
     old = np.arange(c["n"]) >= np.repeat(u.new_counts(c), c["Hq"] // c["Hkv"], 1)[..., None]
     u.check(host(out), np.where(old[..., None], 9.0, want), tol, "out")
     u.check(host(lse), np.where(old, 9.0, want_lse), lse_tol, "lse")
+
+
+@pytest.mark.parametrize("c", [c for c in v.TREES + v.MANY if c["dtype"] == "bf16" and c["Hq"] * c["n"] < 8000], ids=lambda c: f"{c['Hq']}x{c['n']}")
+def test_trees_lose_nothing_to_the_weights(c):
+    _fine(c)
+
+
+@pytest.mark.parametrize("kw,rows", [
+    (dict(n=60, heads=(16, 4), lengths=((2500, 60, 700, 61),), by_head=True), 65536),
+    (dict(kind="empty", n=60, d=64, heads=(16, 4), lengths=((1500,) * 4,), counts=((31,) * 4,)), 131072),
+    (dict(kind="noise", n=250, heads=(4, 4), lengths=((900,) * 4,), pool_token_major=True), 70000)])
+def test_tiles_of_256_columns_in_chunks(kw, rows):
+    _fine(v.tree_case(**dict(dict(page=16), **kw)), rows // 16)

@@ -78,8 +78,10 @@ def test_attention_of_trees(lib_path, i):
     in_child(_tree, lib_path, v.TREES[i])
 
 
-def _tree_fine(path, c):
+def _tree_fine(path, c, entries=0):
     s, want, tol, wl, lt = v.fine(c)
+    more = max(0, entries - s["table"].shape[-1])   # a call that is planned for long lists
+    s["table"] = np.concatenate([s["table"], np.full(s["table"].shape[:-1] + (more,), -1, np.int32)], -1)
     out, lse = _attend(cpu.load(path), c, _fenced(s))
     old = np.arange(c["n"]) >= np.repeat(u.new_counts(c), c["Hq"] // c["Hkv"], 1)[..., None]
     u.check(out, np.where(old[..., None], 9.0, want), tol, "out")
@@ -89,6 +91,11 @@ def _tree_fine(path, c):
 @pytest.mark.parametrize("i", [1, 4, 5, 8, 9, 18, 19])
 def test_trees_lose_nothing_to_the_weights(lib_path, i):
     in_child(_tree_fine, lib_path, v.TREES[i])
+
+
+@pytest.mark.parametrize("d,rows", [(128, 65536), (64, 131072)])
+def test_tiles_of_256_columns_in_chunks(lib_path, d, rows):
+    in_child(_tree_fine, lib_path, v.tree_case("empty", n=60, d=d, heads=(16, 4), lengths=((150, 60, 70, 400),), by_head=True, page=16), rows // 16)
 
 
 def _tree_odd(path, c, kind):
