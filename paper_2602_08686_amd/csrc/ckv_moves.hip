@@ -12,7 +12,8 @@ namespace ckv {
 // reads of its own round and the earlier ones, which a workgroup that takes a list's rows in order has behind a barrier a round. The pieces of a row are
 // independent, so keys, values and parts of rows go to workgroups of their own. Short lists are a chain of four trips to memory (lengths, numbers, pages, rows):
 // seven accepted rows of 16 sequences, 8 heads 3.6 us, up to 544 kept rows of 32 lists 6.7; long ones are bound by what a few workgroups a list have in
-// flight (bf16, 8 lists, 16384 of 32768 rows 64 us, 2.1 TB/s) or by memory (f32, 48 lists, 9362 of 14438 rows 170 us, 4 TB/s of rows read and written).
+// flight (bf16, 8 lists, all of 16384 of 32768 rows 82 us, 134 MB read and written at 1.6 TB/s) or by memory (f32, 48 lists, up to 9362 of 14438 rows 169 us, 692 MB
+// at 4.1 TB/s). Figures with "up to", and those below, are of calls that keep between half of it and all, three quarters on average.
 struct CompactArgs {
   PageLists lists;  // count null: all rows of a list
   char *k, *v;

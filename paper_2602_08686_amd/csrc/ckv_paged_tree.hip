@@ -4,6 +4,7 @@
 // Weights in bf16 enter the second product in two terms, for many columns too, so that a token's result is as near to 64 bits as that of a one-token step.
 // Measured, bf16, 32/8 heads of 128: 16 tokens of 16 sequences over up to 560 rows a head 13.9 us (a token 11.4), 60 tokens, batch 4, 32768 rows 217 us, 593
 // TFLOP/s of the visible pairs' products, 500 tokens, batch 2, 4099 rows 105 us, 566; f32, 14/2 heads of 64, 33 tokens, 1501 rows 18.1 us.
+// 32/8 heads of 64: 60 tokens, batch 4, 32768 rows 151, 500, batch 2, 4099 rows 79; f32, 100 tokens, batch 2, 4099 rows 158 with heads of 128, 85 of 64.
 #include "ckv_paged_few.h"
 #include "ckv_paged_tile.h"
 

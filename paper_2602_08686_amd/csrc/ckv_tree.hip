@@ -12,7 +12,8 @@ constexpr int kTreeThreads = 512;
 constexpr int kTreeStage = 16;  // words of a token that leave LDS together: 128 bytes
 
 // MOST: tokens of a sequence that there is room for. The words go to memory by way of LDS, a token's side by side; written by the lane that finds them, a
-// store touched 64 lines (64 sequences of 1000 tokens 9.4 us, now 6.4).
+// store touched 64 lines (64 sequences of 1000 tokens 9.4 us, now 6.4). Above 1024 tokens a call takes 9.2 us for 16 sequences of 2000, 18.2 for 16 of 4096 (34 MB
+// written: 6.6) and 14.9 for one of 4096, whose eight workgroups each find the paths of all tokens in front of theirs.
 template <int MOST>
 __global__ void __launch_bounds__(kTreeThreads) tree_sees_kernel(const int32_t *parent, const int32_t *start, uint64_t *sees, int32_t *positions, int n) {
   __shared__ uint64_t s_bits[MOST];

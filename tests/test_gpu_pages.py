@@ -32,6 +32,17 @@ def test_tokens_see_their_paths(kind, batch, n):
     assert np.array_equal(positions.cpu(), start[:, None] + depth)
 
 
+@pytest.mark.parametrize("kind", ["star", "odd", "random"])
+@pytest.mark.parametrize("batch,n", [(2, 1025), (1, 2500), (1, 4096)])
+def test_long_trees_that_branch(kind, batch, n):
+    parent = v.parents(kind, batch, n)
+    sees, depth = v.paths(parent)
+    words, positions = torch.full((batch, n, -(-n // 64)), 9, dtype=torch.int64, device=DEV), torch.full((batch, n), 9, dtype=torch.int32, device=DEV)
+    B.ckv_tree_sees(ints(parent), ints(np.arange(batch, dtype=np.int32)), words, positions)
+    torch.cuda.synchronize()
+    assert np.array_equal(words.cpu(), v.words(sees)) and np.array_equal(positions.cpu(), np.arange(batch)[:, None] + depth)
+
+
 def test_the_longest_path():
     parent = v.parents("chain", 2, 4096)
     words = torch.zeros(2, 4096, 64, dtype=torch.int64, device=DEV)

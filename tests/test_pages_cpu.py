@@ -44,6 +44,12 @@ def test_tokens_see_their_paths(lib_path, kind, batch, n):
     in_child(_sees, lib_path, kind, batch, n)
 
 
+@pytest.mark.parametrize("kind", ["star", "odd", "random"])
+@pytest.mark.parametrize("batch,n", [(2, 1025), (1, 2500)])
+def test_long_trees_that_branch(lib_path, kind, batch, n):
+    in_child(_sees, lib_path, kind, batch, n)
+
+
 def test_the_longest_path(lib_path):
     in_child(_sees, lib_path, "chain", 1, 4096)
 
